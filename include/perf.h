@@ -51,7 +51,7 @@ typedef enum {
     PERF_ERR_LAUNCH = 7       /* the HIP runtime reported an error at launch */
 } perf_status;
 
-typedef enum { PERF_F32 = 0, PERF_BF16 = 1 } perf_dtype;
+typedef enum { PERF_F32 = 0, PERF_BF16 = 1, PERF_E4M3 = 2, PERF_E5M2 = 3 } perf_dtype;
 typedef enum { PERF_ROW_MAJOR = 0, PERF_COL_MAJOR = 1 } perf_layout;
 typedef void *perf_stream;
 
@@ -219,6 +219,93 @@ perf_status perf_reduce_mean_ws(const void *x, void *y, void *workspace, int64_t
 typedef enum { PERF_ADD = 0, PERF_MUL = 1, PERF_RELU = 2 } perf_eltwise_op;
 perf_status perf_eltwise(perf_eltwise_op op, const void *a, const void *b, void *y, int64_t n,
                          perf_dtype dt, perf_stream stream);
+
+/* Quantisation to 8-bit floating point with one fp32 scale for each block of 128 elements, the operands of perf_gemm_fp8.
+ * For each block, with F = 448 (PERF_E4M3) or 57344 (PERF_E5M2), the OCP formats' largest finite values:
+ *     s = max(max |x| / F, 2^-126),   q = x * (1/s) rounded to nearest even,     x ~ s * q.
+ *   x       device, rows x cols, row stride ldx, f32 or bf16
+ *   q       row orientation: device, 8-bit, rows x cols, row stride ldq (>= cols), q_dt E4M3 or E5M2
+ *   scales  device fp32; block_rows 1: [rows][ceil(cols/128)], a scale for 128 elements of a row;
+ *           block_rows 128: [ceil(rows/128)][ceil(cols/128)], a scale for a tile; row stride lds
+ *   qt, scales_t  transposed orientation: as q and scales of the cols x rows transpose of x (block_rows 1: blocks of 128
+ *           elements of a column), row strides ldqt (>= rows), ldst.  Either orientation may be left out (both its
+ *           pointers NULL); both come from one read of x.
+ * A linear layer Y = X W^T of X [tokens][in] and W [out][in] takes X by rows and W in tiles (row orientation), its input
+ * gradient dY by rows and W transposed, its weight gradient dY and X transposed by blocks of 1.
+ * A block with an infinity or a NaN reads back (s * q) as NaN where that element is, or everywhere.
+ * Bytes between a row's end and its stride are left as they are.  ldq and ldqt of a multiple of 16 are what perf_gemm_fp8
+ * takes.
+ * Errors: NULL (x, both orientations, or half of one), SHAPE (dimension < 1 or > 2^30, ld too small, block_rows not 1 or
+ * 128), DTYPE, ALIGN (x to its element, scales to 4 bytes), LAUNCH. */
+perf_status perf_quantize_fp8(const void *x, void *q, float *scales, void *qt, float *scales_t, int64_t rows, int64_t cols,
+                              int64_t ldx, int64_t ldq, int64_t lds, int64_t ldqt, int64_t ldst, int64_t block_rows,
+                              perf_dtype x_dt, perf_dtype q_dt, perf_stream stream);
+
+/* Product of block-scaled 8-bit matrices, dense or batched, the 8-bit form of perf_gemm with A row-major and B column-major:
+ *     C_b[m][n] = alpha * sum over blocks j of 128 of K:
+ *                     scaleA_b[m][j] * scaleB_b[n / b_block_rows][j] * sum_{k in block j} A_b[m][k] * B_b[n][k],
+ * products and sums in fp32, one rounding to c_dt.
+ *   A       device, M x K, 8-bit, row stride lda; a_dt E4M3 or E5M2;  scaleA  device fp32, M x ceil(K/128), row stride ldsa
+ *   B       device, N x K, 8-bit, row stride ldb; b_dt E4M3;  scaleB  device fp32, ceil(N / b_block_rows) x ceil(K/128), row
+ *           stride ldsb; b_block_rows 1 (a scale for 128 elements of a row) or 128 (for a tile)
+ *   C       device, M x N, row stride ldc, f32 or bf16
+ *   batch   as in perf_gemm: matrix b starts stride* elements after matrix b-1 (strideSA and strideSB in scales)
+ * The last block may be short; what lies in memory behind a row's K elements is not used.
+ * Errors: NULL, SHAPE (dimension < 1 or > 2^30, ld too small, negative stride, batches overlapping in C, b_block_rows not 1
+ * or 128), DTYPE, ALIGN (A or B not 16-byte aligned, scales or C not aligned to their elements), UNSUPPORTED (b_dt E5M2; lda,
+ * ldb, strideA or strideB not a multiple of 16, or lda or ldb of 2^23 or more), LAUNCH. */
+perf_status perf_gemm_fp8(const void *A, const float *scaleA, const void *B, const float *scaleB, void *C, int64_t M, int64_t N,
+                          int64_t K, int64_t lda, int64_t ldsa, int64_t ldb, int64_t ldsb, int64_t ldc, int64_t b_block_rows,
+                          int64_t batch, int64_t strideA, int64_t strideSA, int64_t strideB, int64_t strideSB, int64_t strideC,
+                          float alpha, perf_dtype a_dt, perf_dtype b_dt, perf_dtype c_dt, perf_stream stream);
+
+/* The RMS norms before and after a block of a network, joined with the block's gate and the scaled residual.  For each row i:
+ *     n = u * r1 * gamma_post,        r1 = 1/sqrt(mean_j u[j]^2 + eps)      (gamma_post NULL: n = u)
+ *     h = residual_scale * x + gate[i / gate_rows] * n                      (gate NULL: 1)
+ *     y = h * r2 * gamma_pre,         r2 = 1/sqrt(mean_j h[j]^2 + eps)
+ * u is the block's output, x the residual stream before it, h the stream behind it and y the next block's input.  Arithmetic
+ * is fp32; h and y are rounded once each (y is computed from h before its rounding).
+ *   u, x, h   device, rows x cols, row strides ldu, ldx, ldh, all of x_dt (f32 or bf16); h may be NULL if y is not
+ *   y         device, rows x cols, row stride ldy, y_dt = x_dt; or y_dt = PERF_E4M3: 8-bit values with a scale for each 128
+ *             elements of a row in y_scales [rows][ceil(cols/128)], row stride lds, as perf_quantize_fp8 of the fp32 y.
+ *             May be NULL if h is not (gamma_pre, y_scales, rrms_pre are then not used)
+ *   gate      device, ceil(rows / gate_rows) x cols, row stride ldg, gate_dt: one for all rows (gate_rows = rows), one of each
+ *             sample's (gate_rows = rows of a sample) or of each element's own (gate_rows = 1); or NULL
+ *   gamma_post, gamma_pre   device, length cols, param_dt
+ *   rrms_post, rrms_pre     device fp32[rows] or NULL: receive r1 and r2, which the gradient takes
+ * h or y may be exactly u or x (same pointer, same stride, same type).
+ * Errors: NULL, SHAPE (rows/cols < 1, cols > 2^30, ld too small, gate_rows < 1, eps < 0 or not finite, residual_scale not
+ * finite), DTYPE, ALIGN (pointer not aligned to its element size), UNSUPPORTED (y_dt neither x_dt nor E4M3), LAUNCH. */
+perf_status perf_residual_norm(const void *u, const void *x, const void *gate, const void *gamma_post, const void *gamma_pre,
+                               void *h, void *y, float *y_scales, float *rrms_post, float *rrms_pre, int64_t rows, int64_t cols,
+                               int64_t ldu, int64_t ldx, int64_t ldg, int64_t gate_rows, int64_t ldh, int64_t ldy, int64_t lds,
+                               float residual_scale, float eps, perf_dtype x_dt, perf_dtype gate_dt, perf_dtype param_dt,
+                               perf_dtype y_dt, perf_stream stream);
+
+/* Gradient of perf_residual_norm.  From dy and dh, the gradients of its y and h (either may be NULL: zero):
+ *     H = dh + r2 * (t - hn * mean_j(t * hn)),   t = dy * gamma_pre,  hn = h * r2;
+ *     dx = residual_scale * H;                   dgamma_pre = sum over rows of dy * hn;
+ *     D = gate * H,  un = u * r1,  v = D * gamma_post:
+ *     du = r1 * (v - un * mean_j(v * un));       dgamma_post = sum over rows of D * un;
+ *     dgate = sum over the rows that share it of un * gamma_post * H;      (gamma_post NULL: du = D, dgate of u * H).
+ * residual_scale is a constant.  Sums are fp32, in an order that the shape alone decides.
+ *   dy, dh, h, u, dx, du    device, rows x cols, of x_dt, row strides lddy .. lddu; h and u as perf_residual_norm took and
+ *                           left them, rrms_post and rrms_pre as it gave them (with gamma_post / dy)
+ *   dgate                   as gate, row stride lddg; dgamma_post, dgamma_pre  device fp32[cols]; each may be NULL: not computed
+ *   workspace               device, at least perf_residual_norm_backward_workspace_bytes(rows, cols) bytes, 4-byte aligned,
+ *                           contents are scratch; calls that may run at the same time need one each
+ * dx may be exactly dh and du exactly dy (same pointer, same stride).  The workspace's size is -1 for arguments that the
+ * call would reject.
+ * Errors: NULL (dy and dh, u, dx, du, workspace; h, gamma_pre or rrms_pre with dy; rrms_post with gamma_post; the gradient of
+ * something not given), SHAPE, DTYPE, ALIGN as perf_residual_norm, LAUNCH. */
+int64_t perf_residual_norm_backward_workspace_bytes(int64_t rows, int64_t cols);
+perf_status perf_residual_norm_backward(const void *dy, const void *dh, const void *h, const void *u, const void *gate,
+                                        const void *gamma_post, const void *gamma_pre, const float *rrms_post,
+                                        const float *rrms_pre, void *dx, void *du, void *dgate, float *dgamma_post,
+                                        float *dgamma_pre, void *workspace, int64_t rows, int64_t cols, int64_t lddy, int64_t lddh,
+                                        int64_t ldh, int64_t ldu, int64_t ldg, int64_t gate_rows, int64_t lddx, int64_t lddu,
+                                        int64_t lddg, float residual_scale, perf_dtype x_dt, perf_dtype gate_dt,
+                                        perf_dtype param_dt, perf_stream stream);
 
 /* The same operators with the kernel variant chosen by the caller instead of by the
  * library's shape rules: the knob a timing-driven search turns (the paper's search scores a

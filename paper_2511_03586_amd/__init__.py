@@ -16,7 +16,7 @@ import os
 PERF_OK = 0
 PERF_ERR_NULL, PERF_ERR_SHAPE, PERF_ERR_DTYPE, PERF_ERR_LAYOUT = 1, 2, 3, 4
 PERF_ERR_ALIGN, PERF_ERR_UNSUPPORTED, PERF_ERR_LAUNCH = 5, 6, 7
-PERF_F32, PERF_BF16 = 0, 1
+PERF_F32, PERF_BF16, PERF_E4M3, PERF_E5M2 = 0, 1, 2, 3
 PERF_ROW_MAJOR, PERF_COL_MAJOR = 0, 1
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -51,6 +51,11 @@ SIGNATURES = {
     "perf_batchnorm_static_max_bytes": (_i64, []),
     "perf_batchnorm_static": (_int, [_ptr, _ptr, _ptr, _ptr, _ptr, _ptr, _i64, _i64, _i64, _i64, _f32, _int, _int, _int,
                                      _ptr]),
+    "perf_quantize_fp8": (_int, [_ptr] * 5 + [_i64] * 8 + [_int, _int, _ptr]),
+    "perf_gemm_fp8": (_int, [_ptr] * 5 + [_i64] * 15 + [_f32, _int, _int, _int, _ptr]),
+    "perf_residual_norm": (_int, [_ptr] * 10 + [_i64] * 9 + [_f32, _f32] + [_int] * 4 + [_ptr]),
+    "perf_residual_norm_backward_workspace_bytes": (_i64, [_i64, _i64]),
+    "perf_residual_norm_backward": (_int, [_ptr] * 15 + [_i64] * 11 + [_f32, _int, _int, _int, _ptr]),
     "perf_copy": (_int, [_ptr, _ptr, _i64, _ptr]),
     "perf_stream_probe": (_int, [_ptr, _ptr, _i64, _int, _int, _int, _i64, _int, _ptr]),
     "perf_mfma_probe": (_int, [_ptr, _i64, _ptr]),
@@ -84,7 +89,8 @@ def lib() -> ctypes.CDLL:
 
 
 _OPERATORS = ("perf_softmax", "perf_layernorm", "perf_gemm", "perf_gemm_softmax", "perf_conv2d", "perf_rmsnorm", "perf_reduce_mean",
-              "perf_reduce_mean_ws", "perf_eltwise", "perf_batchnorm", "perf_batchnorm_static", "perf_copy")
+              "perf_reduce_mean_ws", "perf_eltwise", "perf_batchnorm", "perf_batchnorm_static", "perf_copy",
+              "perf_quantize_fp8", "perf_gemm_fp8", "perf_residual_norm", "perf_residual_norm_backward")
 
 
 class _Native:
@@ -261,6 +267,53 @@ def perf_batchnorm_static(x, gamma, beta, y, mean_out, rstd_out, N, C, H, W, eps
         x, gamma, beta, y, mean_out, rstd_out, N, C, H, W, eps, x_dt, param_dt, y_dt, stream)
     if status and check:
         raise PerfError("perf_batchnorm_static", status)
+    return status
+
+
+def perf_quantize_fp8(x, q, scales, qt, scales_t, rows, cols, ldx, ldq, lds, ldqt, ldst, block_rows=1, x_dt=PERF_BF16,
+                      q_dt=PERF_E4M3, stream=None, check=True) -> int:
+    status = _native.perf_quantize_fp8(
+        x, q, scales, qt, scales_t, rows, cols, ldx, ldq, lds, ldqt, ldst, block_rows, x_dt, q_dt, stream)
+    if status and check:
+        raise PerfError("perf_quantize_fp8", status)
+    return status
+
+
+def perf_gemm_fp8(A, scaleA, B, scaleB, C, M, N, K, lda, ldsa, ldb, ldsb, ldc, b_block_rows=1, batch=1, strideA=0, strideSA=0,
+                  strideB=0, strideSB=0, strideC=0, alpha=1.0, a_dt=PERF_E4M3, b_dt=PERF_E4M3, c_dt=PERF_BF16, stream=None,
+                  check=True) -> int:
+    status = _native.perf_gemm_fp8(
+        A, scaleA, B, scaleB, C, M, N, K, lda, ldsa, ldb, ldsb, ldc, b_block_rows, batch, strideA, strideSA, strideB, strideSB,
+        strideC, alpha, a_dt, b_dt, c_dt, stream)
+    if status and check:
+        raise PerfError("perf_gemm_fp8", status)
+    return status
+
+
+def perf_residual_norm(u, x, gate, gamma_post, gamma_pre, h, y, y_scales, rrms_post, rrms_pre, rows, cols, ldu, ldx, ldg,
+                       gate_rows, ldh, ldy, lds, residual_scale, eps, x_dt=PERF_BF16, gate_dt=PERF_F32, param_dt=PERF_F32,
+                       y_dt=PERF_BF16, stream=None, check=True) -> int:
+    status = _native.perf_residual_norm(
+        u, x, gate, gamma_post, gamma_pre, h, y, y_scales, rrms_post, rrms_pre, rows, cols, ldu, ldx, ldg, gate_rows, ldh, ldy,
+        lds, residual_scale, eps, x_dt, gate_dt, param_dt, y_dt, stream)
+    if status and check:
+        raise PerfError("perf_residual_norm", status)
+    return status
+
+
+def perf_residual_norm_backward_workspace_bytes(rows, cols) -> int:
+    return int(lib().perf_residual_norm_backward_workspace_bytes(rows, cols))
+
+
+def perf_residual_norm_backward(dy, dh, h, u, gate, gamma_post, gamma_pre, rrms_post, rrms_pre, dx, du, dgate, dgamma_post,
+                                dgamma_pre, workspace, rows, cols, lddy, lddh, ldh, ldu, ldg, gate_rows, lddx, lddu, lddg,
+                                residual_scale, x_dt=PERF_BF16, gate_dt=PERF_F32, param_dt=PERF_F32, stream=None,
+                                check=True) -> int:
+    status = _native.perf_residual_norm_backward(
+        dy, dh, h, u, gate, gamma_post, gamma_pre, rrms_post, rrms_pre, dx, du, dgate, dgamma_post, dgamma_pre, workspace, rows,
+        cols, lddy, lddh, ldh, ldu, ldg, gate_rows, lddx, lddu, lddg, residual_scale, x_dt, gate_dt, param_dt, stream)
+    if status and check:
+        raise PerfError("perf_residual_norm_backward", status)
     return status
 
 

@@ -15,24 +15,6 @@
 
 namespace perf {
 
-// Workgroup id -> output tile.  Workgroups are dealt round-robin to the 8 XCDs, each
-// with a private L2, so ids that share an XCD (equal id mod 8) are given a contiguous
-// run of tiles, and runs walk the tile grid in column-major bands of 4 tile-rows: the
-// ~32 tiles an XCD works on at once then form a compact patch sharing A and B panels.
-__device__ __forceinline__ void tile_of_block(int bid, int tiles_m, int tiles_n, int &tm, int &tn)
-{
-    const int total = tiles_m * tiles_n;
-    int id = bid;
-    if (total % 8 == 0) id = (bid % 8) * (total / 8) + bid / 8;
-    constexpr int kBand = 4;
-    const int band_tiles = kBand * tiles_n;
-    const int band = id / band_tiles;
-    const int rows_in_band = min(kBand, tiles_m - band * kBand);
-    const int within = id - band * band_tiles;
-    tm = band * kBand + within % rows_in_band;
-    tn = within / rows_in_band;
-}
-
 template <int TM, int TN, int WM, int WN, bool K64, typename CT, int NS = kStages, bool MI32 = false>
 __global__ __launch_bounds__(64 * WM * WN) void gemm_mfma_kernel(const uint16_t *__restrict__ A,
                                                                  const uint16_t *__restrict__ B, CT *__restrict__ C,

@@ -1,0 +1,419 @@
+// Product of 8-bit matrices with a scale for each block of 128 (perf_gemm_fp8):
+//     C[m][n] = alpha * sum_j scaleA[m][j] * scaleB[n or n / 128][j] * sum_{k in block j} A[m][k] * B[n][k].
+// A block of K is one v_mfma_f32_16x16x128_f8f6f4: its result, started from zero, is scaled on the vector units and added to
+// the fp32 sums.  The rows of B are the instruction's first operand, so that a lane holds four neighbouring n of one m: the
+// scale of A is one value per lane and 16 rows, and C leaves in runs of four.  Which lane holds which k of a block does not
+// matter as long as both operands agree.
+//
+// What the matrix instruction does with a block is less than fp32: of eight products it keeps what reaches down to 2^-13 of
+// the largest and drops the rest before they are added (measured with single products; on normal operands the result is off
+// by 1.3e-5 of its norm, whatever K).  Below the rounding of a bf16 C, 1.6e-3, that does not show.  For an fp32 C the operands
+// are widened to bf16, exactly, and multiplied by v_mfma_f32_16x16x32_bf16, whose sums are fp32 (3e-8): half the rate.
+//
+//  * gemm_fp8_tile_kernel: operands pass through LDS, two stages of one block of K; a workgroup tile of 256 x 256 or less.
+//  * gemm_fp8_waves_kernel: few output tiles or few rows; the waves of a workgroup share one tile and divide the blocks
+//    of K; operands go straight to registers, and the waves' sums are added through LDS in the waves' order.
+#include "fp8.h"
+#include "mfma_tile.h"
+#include "host_utils.h"
+
+namespace perf {
+
+typedef int int8v_t __attribute__((ext_vector_type(8)));
+typedef int int4v_t __attribute__((ext_vector_type(4)));
+
+struct Gemm8Args {
+    const uint8_t *A, *B;
+    const float *sa, *sb;
+    void *C;
+    int M, N, K;
+    int64_t lda, ldsa, ldb, ldsb, ldc, strideA, strideSA, strideB, strideSB, strideC;
+    int64_t batch;
+    int b_block_rows;
+    float alpha;
+};
+
+// A lane's share of 16 rows of an operand in a block, as the matrix instruction takes it: 32 bytes, or with WIDE 32 bf16.
+template <bool WIDE> struct Fragment { int8v_t v; };
+template <> struct Fragment<true> { bf16x8_t v[4]; };
+
+template <bool WIDE, bool E5M2>
+__device__ __forceinline__ Fragment<WIDE> as_fragment(int8v_t v)
+{
+    Fragment<WIDE> f;
+    if constexpr (!WIDE) {
+        f.v = v;
+    } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const int src = v[2 * q + (w >> 1)];
+                typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+                bf16x2_t two;
+                if constexpr (E5M2)
+                    two = (w & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(src, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(src, 1.0f, false);
+                else
+                    two = (w & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(src, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(src, 1.0f, false);
+                f.v[q][2 * w] = two[0], f.v[q][2 * w + 1] = two[1];
+            }
+        }
+    }
+    return f;
+}
+
+// 16 x 16 sums of a block: rows of B (e4m3) by rows of A (e4m3, or e5m2 with A5)
+template <bool WIDE, bool A5>
+__device__ __forceinline__ float4_t mma_block(const Fragment<WIDE> &b, const Fragment<WIDE> &a)
+{
+    float4_t c = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (WIDE) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.v[q], a.v[q], c, 0, 0, 0);
+    } else {
+        c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b.v, a.v, c, 0, A5 ? 1 : 0, 0, 0, 0, 0);
+    }
+    return c;
+}
+
+// Clears the elements of 16 from `n` on.
+__device__ __forceinline__ int4v_t keep_first(int4v_t v, int n)
+{
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const int m = n - 4 * w;
+        v[w] &= m >= 4 ? -1 : m <= 0 ? 0 : (1 << (8 * m)) - 1;
+    }
+    return v;
+}
+
+// An operand's rows as a buffer that ends with the last row's last element, rounded up to whole words (a word that holds an
+// element is readable): what lies behind reads as zero.  Rows of a tile past the matrix read its last row instead.
+__device__ __forceinline__ rsrc_t operand_rsrc(const uint8_t *base, int rows, int64_t ld, int K)
+{
+    return make_rsrc(base, (uint32_t)(((int64_t)(rows - 1) * ld + K + 3) & ~(int64_t)3));
+}
+
+// A lane's 32 elements of a row in a block: the 16 from 16 * (lane / 16) on, and those 64 further on.  `left`: elements of
+// the row from the block's start on; with MASK those behind it are cleared (a row's padding may hold anything).
+template <bool MASK>
+__device__ __forceinline__ int8v_t load_fragment(rsrc_t rsrc, uint32_t row_offset, uint32_t block_offset, int lane, int left)
+{
+    const int k = 16 * (lane >> 4);
+    int4v_t half[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        // (the range check is sure to see the whole offset where it matters: in a short block it is all the lane's)
+        half[h] = __builtin_bit_cast(int4v_t, __builtin_amdgcn_raw_buffer_load_b128(rsrc, row_offset + k + 64 * h + (MASK ? block_offset : 0),
+                                                                                  MASK ? 0 : block_offset, 0));
+        if constexpr (MASK) half[h] = keep_first(half[h], left - (k + 64 * h));
+    }
+    return int8v_t{half[0][0], half[0][1], half[0][2], half[0][3], half[1][0], half[1][1], half[1][2], half[1][3]};
+}
+
+template <typename CT> __device__ __forceinline__ void store_four(CT *p, const float (&v)[4], int n);
+template <> __device__ __forceinline__ void store_four<float>(float *p, const float (&v)[4], int n)
+{
+    if (n >= 4) {
+        __builtin_nontemporal_store(float4_t{v[0], v[1], v[2], v[3]}, reinterpret_cast<float4_at4 *>(p));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (e < n) p[e] = v[e];
+    }
+}
+template <> __device__ __forceinline__ void store_four<uint16_t>(uint16_t *p, const float (&v)[4], int n)
+{
+    if (n >= 4) {
+        *reinterpret_cast<uint2_at2 *>(p) = uint2_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (e < n) p[e] = f32_to_bf16(v[e]);
+    }
+}
+
+// TM x TN groups of 16 rows of A and of B per workgroup; W waves, wave w takes the blocks w, w + W, ...
+template <int TM, int TN, int W, bool A5, typename CT>
+__global__ __launch_bounds__(64 * W) void gemm_fp8_waves_kernel(const Gemm8Args g, int tiles_m)
+{
+    __shared__ float4_t sums[W][TM * TN][64];
+    constexpr bool WIDE = sizeof(CT) == 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t bz = blockIdx.y;
+    const int tile_m = (int)blockIdx.x % tiles_m, tile_n = (int)blockIdx.x / tiles_m;
+    const int m0 = tile_m * 16 * TM, n0 = tile_n * 16 * TN;
+    const int rows_m = min(16 * TM, g.M - m0), rows_n = min(16 * TN, g.N - n0);
+    const int blocks = (g.K + kBlock8 - 1) / kBlock8;
+    const rsrc_t ra = operand_rsrc(g.A + bz * g.strideA + (int64_t)m0 * g.lda, rows_m, g.lda, g.K);
+    const rsrc_t rb = operand_rsrc(g.B + bz * g.strideB + (int64_t)n0 * g.ldb, rows_n, g.ldb, g.K);
+    const float *sa = g.sa + bz * g.strideSA, *sb = g.sb + bz * g.strideSB;
+    uint32_t a_off[TM], b_off[TN];
+    const float *sa_row[TM], *sb_row[TN][4];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int r = min(16 * i + (lane & 15), rows_m - 1);
+        a_off[i] = (uint32_t)(r * g.lda);
+        sa_row[i] = sa + (int64_t)(m0 + r) * g.ldsa;
+    }
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        b_off[j] = (uint32_t)(min(16 * j + (lane & 15), rows_n - 1) * g.ldb);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int n = n0 + min(16 * j + 4 * (lane >> 4) + e, rows_n - 1);
+            sb_row[j][e] = sb + (int64_t)(n / g.b_block_rows) * g.ldsb;
+        }
+    }
+    float4_t acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = float4_t{0.f, 0.f, 0.f, 0.f};
+    auto block = [&](int kb, auto mask) {
+        constexpr bool MASK = decltype(mask)::value;
+        const int left = g.K - kb * kBlock8;
+        int8v_t ra_[TM], rb_[TN];
+        float fa[TM], fb[TN][4];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) ra_[i] = load_fragment<MASK>(ra, a_off[i], (uint32_t)kb * kBlock8, lane, left), fa[i] = sa_row[i][kb];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            rb_[j] = load_fragment<MASK>(rb, b_off[j], (uint32_t)kb * kBlock8, lane, left);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) fb[j][e] = sb_row[j][e][kb];
+        }
+        Fragment<WIDE> a[TM], b[TN];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) a[i] = as_fragment<WIDE, A5>(ra_[i]);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) b[j] = as_fragment<WIDE, false>(rb_[j]);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const float4_t p = mma_block<WIDE, A5>(b[j], a[i]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_fmaf(p[e] * fa[i], fb[j][e], acc[i][j][e]);
+            }
+    };
+    const int whole = g.K / kBlock8;
+    int kb = wave;
+    for (; kb < whole; kb += W) block(kb, std::false_type{});
+    if (kb < blocks) block(kb, std::true_type{});
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) sums[wave][i * TN + j][lane] = acc[i][j];
+    __syncthreads();
+    CT *C = (CT *)g.C + bz * g.strideC;
+    for (int t = wave; t < TM * TN; t += W) {
+        const int i = t / TN, j = t - i * TN;
+        float4_t s = sums[0][t][lane];
+#pragma unroll
+        for (int w = 1; w < W; ++w) s += sums[w][t][lane];
+        const int m = m0 + 16 * i + (lane & 15), n = n0 + 16 * j + 4 * (lane >> 4);
+        const float v[4] = {g.alpha * s[0], g.alpha * s[1], g.alpha * s[2], g.alpha * s[3]};
+        if (m < g.M) store_four<CT>(C + (int64_t)m * g.ldc + n, v, g.N - n);
+    }
+}
+
+// WM x WN waves, each with TM x TN groups of 16 rows of A and of B.  LDS: two stages of a block of K, rows of 128 bytes whose
+// 16-byte chunks are permuted as in mfma_tile.h (swz64), and the block's scales.  A step waits for its stage, which had the
+// whole step before to arrive, starts the loads of the next, and multiplies: B's fragments stay in registers, A's pass by.
+template <int TM, int TN, int WM, int WN, bool B128, bool A5, typename CT>
+__global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Gemm8Args g, int tiles_m, int tiles_n)
+{
+    constexpr bool WIDE = sizeof(CT) == 4;
+    constexpr int NW = WM * WN, BM = 16 * TM * WM, BN = 16 * TN * WN;
+    constexpr int kStage = (BM + BN) * kBlock8, kLoadsA = BM / (8 * NW), kLoadsB = BN / (8 * NW);
+    constexpr int kScales = B128 ? BM : BM + BN;  // of a stage; a wave fetches 64 of them
+    static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && kScales <= 64 * NW && kScales % 64 == 0, "the loads divide among the waves");
+    __shared__ __attribute__((aligned(1024))) char smem[2 * kStage];
+    __shared__ __attribute__((aligned(16))) float scales[2][kScales];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+    const int64_t bz = blockIdx.y;
+    int tm, tn;
+    tile_of_block(blockIdx.x, tiles_m, tiles_n, tm, tn);
+    const int m0 = tm * BM, n0 = tn * BN;
+    const int rows_m = min(BM, g.M - m0), rows_n = min(BN, g.N - n0);
+    const int blocks = (g.K + kBlock8 - 1) / kBlock8;
+    const rsrc_t ra = operand_rsrc(g.A + bz * g.strideA + (int64_t)m0 * g.lda, rows_m, g.lda, g.K);
+    const rsrc_t rb = operand_rsrc(g.B + bz * g.strideB + (int64_t)n0 * g.ldb, rows_n, g.ldb, g.K);
+    // this lane's row and chunk in each of its wave's loads of 8 rows; the offset moves on by a block per step
+    uint32_t off[kLoadsA + kLoadsB];
+#pragma unroll
+    for (int i = 0; i < kLoadsA + kLoadsB; ++i) {
+        const bool is_a = i < kLoadsA;
+        const int row = ((is_a ? i : i - kLoadsA) * NW + wave) * 8 + (lane >> 3);
+        off[i] = (uint32_t)(min(row, (is_a ? rows_m : rows_n) - 1) * (is_a ? g.lda : g.ldb)) + (((lane & 7) ^ swz64(row)) << 4);
+    }
+    const float *my_scale = nullptr;  // the row of scales that this lane fetches for all
+    if (wave * 64 < kScales) {
+        const int s = wave * 64 + lane;
+        if (s < BM)
+            my_scale = g.sa + bz * g.strideSA + (int64_t)(m0 + min(s, rows_m - 1)) * g.ldsa;
+        else
+            my_scale = g.sb + bz * g.strideSB + (int64_t)(n0 + min(s - BM, rows_n - 1)) * g.ldsb;
+    }
+    const float *sb128 = g.sb + bz * g.strideSB + (int64_t)min((n0 + wn * 16 * TN) / kBlock8, (g.N - 1) / kBlock8) * g.ldsb;
+
+    auto issue = [&](int kb) {
+        char *stage = smem + (kb & 1) * kStage;
+#pragma unroll
+        for (int i = 0; i < kLoadsA + kLoadsB; ++i) {
+            const bool is_a = i < kLoadsA;
+            issue_load_to(is_a ? ra : rb, off[i], 0, stage + (is_a ? 0 : BM * kBlock8) + ((is_a ? i : i - kLoadsA) * NW + wave) * 1024);
+            off[i] += kBlock8;
+        }
+    };
+    float4_t acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = float4_t{0.f, 0.f, 0.f, 0.f};
+
+    auto read = [&](const char *rows, int row, auto mask, int left) {
+        constexpr bool MASK = decltype(mask)::value;
+        int4v_t half[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int chunk = (lane >> 4) + 4 * h;
+            half[h] = *reinterpret_cast<const int4v_t *>(rows + frag_offset64(row + (lane & 15), chunk));
+            if constexpr (MASK) half[h] = keep_first(half[h], left - 16 * chunk);
+        }
+        return int8v_t{half[0][0], half[0][1], half[0][2], half[0][3], half[1][0], half[1][1], half[1][2], half[1][3]};
+    };
+    float next_scale = my_scale ? my_scale[0] : 0.f, next128 = B128 ? sb128[0] : 0.f;
+    auto step = [&](int kb, auto mask) {
+        if (my_scale) scales[kb & 1][wave * 64 + lane] = next_scale;
+        const float s128 = next128;
+        wait_vmem_and_lds<0>();  // this wave's share of the stage has landed, and its scales
+        wg_barrier();            // everyone's; and everyone has left the other stage
+        if (kb + 1 < blocks) {
+            issue(kb + 1);
+            if (my_scale) next_scale = my_scale[kb + 1];
+            if constexpr (B128) next128 = sb128[kb + 1];
+        }
+        const char *rows_a = smem + (kb & 1) * kStage, *rows_b = rows_a + BM * kBlock8;
+        const float *sa = scales[kb & 1] + wm * 16 * TM;
+        const int left = g.K - kb * kBlock8;
+        Fragment<WIDE> b[TN];
+        float4_t fb[TN];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            b[j] = as_fragment<WIDE, false>(read(rows_b, wn * 16 * TN + 16 * j, mask, left));
+            if constexpr (!B128) fb[j] = *reinterpret_cast<const float4_t *>(scales[kb & 1] + BM + wn * 16 * TN + 16 * j + 4 * (lane >> 4));
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const Fragment<WIDE> a = as_fragment<WIDE, A5>(read(rows_a, wm * 16 * TM + 16 * i, mask, left));
+            const float fa = sa[16 * i + (lane & 15)];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const float4_t p = mma_block<WIDE, A5>(b[j], a);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float f = s128;
+                    if constexpr (!B128) f = fb[j][e];
+                    acc[i][j][e] = __builtin_fmaf(p[e] * fa, f, acc[i][j][e]);
+                }
+            }
+        }
+    };
+    issue(0);
+    const int whole = g.K / kBlock8;
+    for (int kb = 0; kb < whole; ++kb) step(kb, std::false_type{});
+    if (whole < blocks) step(whole, std::true_type{});
+
+    CT *C = (CT *)g.C + bz * g.strideC;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int m = m0 + wm * 16 * TM + 16 * i + (lane & 15);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const int n = n0 + wn * 16 * TN + 16 * j + 4 * (lane >> 4);
+            const float v[4] = {g.alpha * acc[i][j][0], g.alpha * acc[i][j][1], g.alpha * acc[i][j][2], g.alpha * acc[i][j][3]};
+            if (m < g.M) store_four<CT>(C + (int64_t)m * g.ldc + n, v, g.N - n);
+        }
+    }
+}
+
+template <int TM, int TN, int WM, int WN, bool A5, typename CT>
+static perf_status launch_tile(const Gemm8Args &g, hipStream_t stream)
+{
+    const int64_t tiles_m = (g.M + 16 * TM * WM - 1) / (16 * TM * WM), tiles_n = (g.N + 16 * TN * WN - 1) / (16 * TN * WN);
+    if (tiles_m * tiles_n > max_blocks(64 * WM * WN)) return PERF_ERR_UNSUPPORTED;
+    for (int64_t b = 0; b < g.batch; b += kMaxGridYZ) {
+        Gemm8Args p = g;
+        p.A += b * g.strideA, p.B += b * g.strideB, p.sa += b * g.strideSA, p.sb += b * g.strideSB;
+        p.C = (CT *)g.C + b * g.strideC;
+        const dim3 grid((unsigned)(tiles_m * tiles_n), (unsigned)std::min(kMaxGridYZ, g.batch - b));
+        if (g.b_block_rows == kBlock8)
+            gemm_fp8_tile_kernel<TM, TN, WM, WN, true, A5, CT><<<grid, 64 * WM * WN, 0, stream>>>(p, (int)tiles_m, (int)tiles_n);
+        else
+            gemm_fp8_tile_kernel<TM, TN, WM, WN, false, A5, CT><<<grid, 64 * WM * WN, 0, stream>>>(p, (int)tiles_m, (int)tiles_n);
+        const perf_status st = launch_status();
+        if (st != PERF_OK) return st;
+    }
+    return PERF_OK;
+}
+
+template <int TM, int TN, int W, bool A5, typename CT>
+static perf_status launch_waves(const Gemm8Args &g, hipStream_t stream)
+{
+    const int64_t tiles_m = (g.M + 16 * TM - 1) / (16 * TM), tiles_n = (g.N + 16 * TN - 1) / (16 * TN);
+    if (tiles_m * tiles_n > max_blocks(64 * W)) return PERF_ERR_UNSUPPORTED;
+    for (int64_t b = 0; b < g.batch; b += kMaxGridYZ) {
+        Gemm8Args p = g;
+        p.A += b * g.strideA, p.B += b * g.strideB, p.sa += b * g.strideSA, p.sb += b * g.strideSB;
+        p.C = (CT *)g.C + b * g.strideC;
+        const dim3 grid((unsigned)(tiles_m * tiles_n), (unsigned)std::min(kMaxGridYZ, g.batch - b));
+        gemm_fp8_waves_kernel<TM, TN, W, A5, CT><<<grid, 64 * W, 0, stream>>>(p, (int)tiles_m);
+        const perf_status st = launch_status();
+        if (st != PERF_OK) return st;
+    }
+    return PERF_OK;
+}
+
+template <bool A5, typename CT>
+static perf_status gemm8(const Gemm8Args &g, hipStream_t stream)
+{
+    const int64_t big = ((g.M + 255) / 256) * ((g.N + 255) / 256) * g.batch, mid = ((g.M + 127) / 128) * ((g.N + 127) / 128) * g.batch;
+    if constexpr (sizeof(CT) == 2) {
+        if (big >= 200) return launch_tile<8, 4, 2, 4, A5, CT>(g, stream);
+    }
+    if (mid >= 200) return launch_tile<4, 4, 2, 2, A5, CT>(g, stream);
+    if (g.M <= 16) return launch_waves<1, 1, 8, A5, CT>(g, stream);
+    return launch_waves<2, 2, 8, A5, CT>(g, stream);
+}
+
+}  // namespace perf
+
+extern "C" perf_status perf_gemm_fp8(const void *A, const float *scaleA, const void *B, const float *scaleB, void *C, int64_t M,
+                                     int64_t N, int64_t K, int64_t lda, int64_t ldsa, int64_t ldb, int64_t ldsb, int64_t ldc,
+                                     int64_t b_block_rows, int64_t batch, int64_t strideA, int64_t strideSA, int64_t strideB,
+                                     int64_t strideSB, int64_t strideC, float alpha, perf_dtype a_dt, perf_dtype b_dt,
+                                     perf_dtype c_dt, perf_stream stream)
+{
+    using namespace perf;
+    if (!A || !scaleA || !B || !scaleB || !C) return PERF_ERR_NULL;
+    if (M < 1 || N < 1 || K < 1 || batch < 1 || M > kMaxExtent8 || N > kMaxExtent8 || K > kMaxExtent8) return PERF_ERR_SHAPE;
+    const int64_t blocks = (K + kBlock8 - 1) / kBlock8;
+    if (lda < K || ldb < K || ldsa < blocks || ldsb < blocks || ldc < N) return PERF_ERR_SHAPE;
+    if (b_block_rows != 1 && b_block_rows != kBlock8) return PERF_ERR_SHAPE;
+    if (strideA < 0 || strideSA < 0 || strideB < 0 || strideSB < 0 || strideC < 0) return PERF_ERR_SHAPE;
+    if (batch > 1 && strideC < (M - 1) * ldc + N) return PERF_ERR_SHAPE;
+    if (!dtype8_ok(a_dt) || !dtype8_ok(b_dt) || !dtype_ok(c_dt)) return PERF_ERR_DTYPE;
+    if (!aligned(A, 16) || !aligned(B, 16) || !aligned(scaleA, 4) || !aligned(scaleB, 4) || !aligned(C, dtype_size(c_dt)))
+        return PERF_ERR_ALIGN;
+    if (b_dt != PERF_E4M3 || lda % 16 || ldb % 16 || lda >= (1 << 23) || ldb >= (1 << 23)) return PERF_ERR_UNSUPPORTED;
+    if (batch > 1 && (strideA % 16 || strideB % 16)) return PERF_ERR_UNSUPPORTED;
+    const Gemm8Args g{(const uint8_t *)A, (const uint8_t *)B, scaleA, scaleB, C, (int)M, (int)N, (int)K, lda, ldsa, ldb, ldsb, ldc,
+                      strideA, strideSA, strideB, strideSB, strideC, batch, (int)b_block_rows, alpha};
+    const hipStream_t st = (hipStream_t)stream;
+    const bool a5 = a_dt == PERF_E5M2;
+    if (c_dt == PERF_BF16) return a5 ? gemm8<true, uint16_t>(g, st) : gemm8<false, uint16_t>(g, st);
+    return a5 ? gemm8<true, float>(g, st) : gemm8<false, float>(g, st);
+}

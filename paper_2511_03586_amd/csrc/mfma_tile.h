@@ -252,6 +252,24 @@ __device__ __forceinline__ void mfma_mainloop(WaveTile<TM, TN> &t, char *smem, i
     wait_vmem_and_lds<0>();  // drain the over-issued loads and reads before LDS is reused or released
 }
 
+// Workgroup id -> output tile.  Workgroups are dealt round-robin to the 8 XCDs, each
+// with a private L2, so ids that share an XCD (equal id mod 8) are given a contiguous
+// run of tiles, and runs walk the tile grid in column-major bands of 4 tile-rows: the
+// ~32 tiles an XCD works on at once then form a compact patch sharing A and B panels.
+__device__ __forceinline__ void tile_of_block(int bid, int tiles_m, int tiles_n, int &tm, int &tn)
+{
+    const int total = tiles_m * tiles_n;
+    int id = bid;
+    if (total % 8 == 0) id = (bid % 8) * (total / 8) + bid / 8;
+    constexpr int kBand = 4;
+    const int band_tiles = kBand * tiles_n;
+    const int band = id / band_tiles;
+    const int rows_in_band = min(kBand, tiles_m - band * kBand);
+    const int within = id - band * band_tiles;
+    tm = band * kBand + within % rows_in_band;
+    tn = within / rows_in_band;
+}
+
 template <typename CT> __device__ __forceinline__ void store_c(CT *p, float v);
 // C is written once and not re-read by the kernel: stream it past the caches.
 template <> __device__ __forceinline__ void store_c<float>(float *p, float v) { __builtin_nontemporal_store(v, p); }
