@@ -274,7 +274,7 @@ perf_status perf_gemm_fp8(const void *A, const float *scaleA, const void *B, con
  *   gamma_post, gamma_pre   device, length cols, param_dt
  *   rrms_post, rrms_pre     device fp32[rows] or NULL: receive r1 and r2, which the gradient takes
  * h or y may be exactly u or x (same pointer, same stride, same type).
- * Errors: NULL, SHAPE (rows/cols < 1, cols > 2^30, ld too small, gate_rows < 1, eps < 0 or not finite, residual_scale not
+ * Errors: NULL, SHAPE (rows/cols < 1 or > 2^30, ld too small, gate_rows < 1, eps < 0 or not finite, residual_scale not
  * finite), DTYPE, ALIGN (pointer not aligned to its element size), UNSUPPORTED (y_dt neither x_dt nor E4M3), LAUNCH. */
 perf_status perf_residual_norm(const void *u, const void *x, const void *gate, const void *gamma_post, const void *gamma_pre,
                                void *h, void *y, float *y_scales, float *rrms_post, float *rrms_pre, int64_t rows, int64_t cols,

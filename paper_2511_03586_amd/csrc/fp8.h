@@ -2,6 +2,7 @@
 // value 448, no infinities) and e5m2 (largest finite value 57344), blocks of 128 elements with one fp32 scale, and
 // groups of 8 elements of a row as a lane holds them.
 #pragma once
+#include <type_traits>
 #include "row_io.h"
 
 namespace perf {
@@ -11,6 +12,7 @@ constexpr int kBlock8 = 128;  // elements of a row that share a scale
 typedef uint32_t uint4_at1 __attribute__((ext_vector_type(4), aligned(1)));
 typedef uint32_t uint4_at4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t uint2_at1 __attribute__((ext_vector_type(2), aligned(1)));
+typedef uint32_t uint32_at1 __attribute__((aligned(1)));
 
 template <bool E5M2> struct Fp8 {
     static constexpr float kLargest = E5M2 ? 57344.f : 448.f;
@@ -36,7 +38,7 @@ template <bool E5M2> struct Fp8 {
     }
 };
 
-// Largest of an unsigned value over groups of 8 or 16 neighbouring lanes.
+// Largest of an unsigned value over groups of 8, 16 or 32 neighbouring lanes.
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp_max_u32(uint32_t v)
 {
@@ -46,11 +48,16 @@ __device__ __forceinline__ uint32_t dpp_max_u32(uint32_t v)
 template <int LANES>
 __device__ __forceinline__ uint32_t group_max_u32(uint32_t v)
 {
-    static_assert(LANES == 8 || LANES == 16, "a DPP row or half of one");
+    static_assert(LANES == 8 || LANES == 16 || LANES == 32, "half a DPP row, one, or two");
     v = dpp_max_u32<0xB1>(v);   // quad_perm [1,0,3,2]
     v = dpp_max_u32<0x4E>(v);   // quad_perm [2,3,0,1]
     v = dpp_max_u32<0x141>(v);  // row_half_mirror
-    if constexpr (LANES == 16) v = dpp_max_u32<0x140>(v);  // row_mirror
+    if constexpr (LANES >= 16) v = dpp_max_u32<0x140>(v);  // row_mirror
+    if constexpr (LANES == 32) {
+        const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        const uint32_t p0 = p[0], p1 = p[1];
+        v = max(p0, p1);
+    }
     return v;
 }
 
@@ -69,11 +76,6 @@ template <> struct Eight<uint16_t> {
             asm("" : "+v"(w));
             raw[e] = w;
         }
-    }
-    __device__ __forceinline__ void keep(bool in)  // or zeros
-    {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) raw[e] = in ? raw[e] : 0u;
     }
     __device__ __forceinline__ void load(const uint16_t *p, int n)  // (read once: past the caches)
     {
@@ -115,11 +117,6 @@ template <> struct Eight<float> {
             asm("" : "+v"(w), "+v"(v));
             lo[e] = w, hi[e] = v;
         }
-    }
-    __device__ __forceinline__ void keep(bool in)
-    {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) lo[e] = in ? lo[e] : 0u, hi[e] = in ? hi[e] : 0u;
     }
     __device__ __forceinline__ void load(const float *p, int n)
     {
@@ -172,37 +169,8 @@ __device__ __forceinline__ void store_eight(T *p, const float (&v)[8], int n)
 template <typename T>
 __device__ __forceinline__ T *offset_by(T *row, int c)
 {
-    return reinterpret_cast<T *>(reinterpret_cast<uintptr_t>(row) + (uint32_t)c * (uint32_t)sizeof(T));
-}
-
-// A group of a row at element c, n = cols - c: RAG takes any number of columns; without it there are whole groups only, and
-// one behind the row's end loads the row's first instead, to be masked later: a load on one of two paths of a loop would
-// make the compiler wait for all that are in flight.
-template <bool RAG, typename T>
-__device__ __forceinline__ void load_group(Eight<T> &g, const T *row, int c, int n)
-{
-    if constexpr (RAG)
-        g.load(row + c, n);
-    else
-        g.load(offset_by(row, n > 0 ? c : 0), 8);
-}
-// ... and its way back: nothing is written of what lies behind the row's end
-template <bool RAG, typename T>
-__device__ __forceinline__ void store_group(T *row, const float (&v)[8], int c, int n)
-{
-    if constexpr (RAG) {
-        store_eight(row + c, v, n);
-    } else {
-        if (n > 0) store_row_chunk<true, T, 8>(offset_by(row, c), v);
-    }
-}
-// ... as fp32, zeros unless `in`
-template <typename T>
-__device__ __forceinline__ void get_group(const Eight<T> &g, float (&v)[8], bool in)
-{
-    g.get(v);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = in ? v[e] : 0.f;
+    using Byte = std::conditional_t<std::is_const_v<T>, const char, char>;
+    return reinterpret_cast<T *>(reinterpret_cast<Byte *>(row) + (uint32_t)c * (uint32_t)sizeof(T));
 }
 
 // N bytes (8 or 16), n of them inside the row, at any address
@@ -220,6 +188,96 @@ __device__ __forceinline__ void store_bytes(uint8_t *p, const uint32_t (&w)[N / 
             if (e < n) p[e] = (uint8_t)(w[e >> 2] >> (8 * (e & 3)));
     }
 }
+
+// Where a lane's eight elements lie in rows of at least eight: one run of eight (bf16) or two of four (fp32, so that a load
+// of a wave is one run of memory), the runs of `threads` lanes side by side.  The run that would overhang the row (RAG)
+// starts as many elements before its end instead; its first `dup` elements are its neighbour's too: computed by both, left out
+// of sums over the row and stored by the neighbour.  Runs behind the row load others' elements and drop them: a load on one
+// of two paths of a loop would make the compiler wait for all that are in flight.
+template <typename T, bool RAG> struct Group {
+    static constexpr int kRuns = sizeof(T) / 2, kRun = 8 / kRuns;
+    int at[kRuns], dup[kRuns];
+    __device__ __forceinline__ Group(int lane, int threads, int cols)
+    {
+#pragma unroll
+        for (int r = 0; r < kRuns; ++r) {
+            const int c = kRun * (lane + r * threads);
+            at[r] = RAG ? min(c, cols - kRun) : c < cols ? c : 0;
+            dup[r] = RAG ? c - at[r] : c < cols ? 0 : kRun;
+        }
+    }
+    __device__ __forceinline__ bool in(int e) const { return dup[e / kRun] < kRun; }  // whether the run of element e is in the row
+    __device__ __forceinline__ float once(int e, float v) const { return !RAG || e % kRun >= dup[e / kRun] ? v : 0.f; }
+    __device__ __forceinline__ void load(Eight<T> &g, const T *row) const  // (read once: past the caches)
+    {
+        if constexpr (kRuns == 1) {
+            g.raw = __builtin_nontemporal_load(reinterpret_cast<const uint4_at2 *>(offset_by(row, at[0])));
+        } else {
+            g.lo = __builtin_nontemporal_load(reinterpret_cast<const uint4_at4 *>(offset_by(row, at[0])));
+            g.hi = __builtin_nontemporal_load(reinterpret_cast<const uint4_at4 *>(offset_by(row, at[1])));
+        }
+    }
+    __device__ __forceinline__ void keep(Eight<T> &g, bool in_row) const  // or zeros
+    {
+        if constexpr (kRuns == 1)
+            g.raw = in_row && in(0) ? g.raw : uint4_t{0, 0, 0, 0};
+        else
+            g.lo = in_row && in(0) ? g.lo : uint4_t{0, 0, 0, 0}, g.hi = in_row && in(4) ? g.hi : uint4_t{0, 0, 0, 0};
+    }
+    // the same elements of another row, of any type, as fp32; zeros behind the row's end
+    template <typename P>
+    __device__ __forceinline__ void load_as(const P *row, float (&v)[8]) const
+    {
+        typedef P Some __attribute__((ext_vector_type(kRun), aligned(sizeof(P))));
+#pragma unroll
+        for (int r = 0; r < kRuns; ++r) {
+            const Some w = *reinterpret_cast<const Some *>(offset_by(row, at[r]));
+#pragma unroll
+            for (int e = 0; e < kRun; ++e) {
+                const P one = w[e];
+                v[kRun * r + e] = in(kRun * r) ? Elem<P>::load1(&one) : 0.f;
+            }
+        }
+    }
+    template <typename P>
+    __device__ __forceinline__ void store(P *row, const float (&v)[8]) const
+    {
+#pragma unroll
+        for (int r = 0; r < kRuns; ++r) {
+            P *p = offset_by(row, at[r]);
+            const float *f = v + kRun * r;
+            if (dup[r] == 0) {
+                if constexpr (kRun == 8) {
+                    store_row_chunk<true, P, 8>(p, f);
+                } else {
+                    store_row_chunk<true, P, 4>(p, f);
+                }
+            } else if constexpr (RAG) {
+#pragma unroll
+                for (int e = 1; e < kRun; ++e)
+                    if (e >= dup[r]) Elem<P>::store1(p + e, f[e]);
+            }
+        }
+    }
+    // the eight as bytes w
+    __device__ __forceinline__ void store_bytes(uint8_t *row, const uint32_t (&w)[2]) const
+    {
+#pragma unroll
+        for (int r = 0; r < kRuns; ++r) {
+            uint8_t *p = offset_by(row, at[r]);
+            if (dup[r] == 0) {
+                if constexpr (kRun == 8)
+                    *reinterpret_cast<uint2_at1 *>(p) = uint2_t{w[0], w[1]};
+                else
+                    *reinterpret_cast<uint32_at1 *>(p) = w[r];
+            } else if constexpr (RAG) {
+#pragma unroll
+                for (int e = 1; e < kRun; ++e)
+                    if (e >= dup[r]) p[e] = (uint8_t)(w[(kRun * r + e) >> 2] >> (8 * (e & 3)));
+            }
+        }
+    }
+};
 
 // Magnitude bits of a value as they are compared for a block's largest
 __device__ __forceinline__ uint32_t magnitude(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }

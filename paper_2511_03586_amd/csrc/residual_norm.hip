@@ -7,9 +7,9 @@
 //     D = gate H,  v = D gamma_post,     du = r1 (v - un mean(v un)),  dgamma_post = sum of D un,  dgate = sum of n H.
 // (gamma_post left out: n = u, du = D.)  Bound by HBM: each operand is read once and each result written once.
 //
-//  * residual_norm_kernel / residual_norm_grad_kernel<W, NC>: W waves own a row, NC groups of 8 elements per lane, so that
-//    a row is in registers between its two sums; 8 / W rows side by side in a workgroup of 8 waves.  The gains and the
-//    gate stay in registers for all rows that share them.
+//  * residual_norm_kernel / residual_norm_grad_kernel<W>: W waves own a row, 8 elements per lane, so that a row is in
+//    registers between its two sums; workgroups of 8 waves (gradient: 16) take the rows of several teams side by side.  The gains and the gate are read
+//    once for all rows that share them.
 //  * The gradient's sums over rows: a workgroup owns a run of rows and sums them in registers; its sums go to the
 //    workspace and are added in the order of the rows by residual_norm_sums_kernel.  No atomics.
 //  * residual_norm_any_kernel and its gradient: rows beyond 16 waves' registers, several passes over memory.
@@ -27,25 +27,35 @@ struct Param {
     {
         return bf16 ? bf16_to_f32(reinterpret_cast<const uint16_t *>(p)[j]) : reinterpret_cast<const float *>(p)[j];
     }
-    // n of the eight elements from j on, the others zero; RAG as for rows
-    template <bool RAG = true>
+    // n of the eight elements from j on, the others zero
     __device__ __forceinline__ void eight(int64_t j, int n, float (&v)[8]) const
     {
-        if constexpr (!RAG) j = n > 0 ? j : 0, n = n > 0 ? 8 : 0;
         if (bf16) {
             Eight<uint16_t> e;
-            e.load_cached(reinterpret_cast<const uint16_t *>(p) + j, RAG ? n : 8);
-            get_group(e, v, RAG || n > 0);
+            e.load_cached(reinterpret_cast<const uint16_t *>(p) + j, n);
+            e.get(v);
         } else {
             Eight<float> e;
-            e.load_cached(reinterpret_cast<const float *>(p) + j, RAG ? n : 8);
-            get_group(e, v, RAG || n > 0);
+            e.load_cached(reinterpret_cast<const float *>(p) + j, n);
+            e.get(v);
         }
     }
-    __device__ __forceinline__ void four(int64_t j, int n, float (&v)[4]) const
+    // a lane's group of the row that begins at `row`
+    template <typename G>
+    __device__ __forceinline__ void group(int64_t row, const G &at, float (&v)[8]) const
     {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = e < n ? at(j + e) : 0.f;
+        if (bf16)
+            at.load_as(reinterpret_cast<const uint16_t *>(p) + row, v);
+        else
+            at.load_as(reinterpret_cast<const float *>(p) + row, v);
+    }
+    template <typename G>
+    __device__ __forceinline__ void put_group(int64_t row, const G &at, const float (&v)[8]) const
+    {
+        if (bf16)
+            at.store(reinterpret_cast<uint16_t *>(const_cast<void *>(p)) + row, v);
+        else
+            at.store(reinterpret_cast<float *>(const_cast<void *>(p)) + row, v);
     }
     __device__ __forceinline__ void put(int64_t j, float v) const
     {
@@ -54,14 +64,6 @@ struct Param {
         else
             reinterpret_cast<float *>(const_cast<void *>(p))[j] = v;
     }
-    template <bool RAG>
-    __device__ __forceinline__ void put_eight(int64_t at, const float (&v)[8], int c, int n) const
-    {
-        if (bf16)
-            store_group<RAG>(reinterpret_cast<uint16_t *>(const_cast<void *>(p)) + at, v, c, n);
-        else
-            store_group<RAG>(reinterpret_cast<float *>(const_cast<void *>(p)) + at, v, c, n);
-    }
 };
 
 struct NormArgs {
@@ -69,8 +71,9 @@ struct NormArgs {
     Param gate, post, pre;  // p is null where there is none
     void *h, *y;
     float *y_scales, *r_post, *r_pre;
-    int64_t rows, ldu, ldx, ldg, gate_rows, ldh, ldy, lds;
-    int cols;
+    int64_t ldu, ldx, ldg, ldh, ldy, lds;
+    int rows, cols, gate_rows;
+    uint32_t gate_magic;  // of a division by gate_rows: one of 64 bits runs on the vector units, and every row's address behind it
     float residual_scale, eps;
 };
 
@@ -92,8 +95,8 @@ __device__ __forceinline__ float team_sum(float v, float *red)
     return v;
 }
 
-// Y8: y is e4m3 with scales (else of x's type)
-template <typename T, int W, int NC, bool Y8, bool RAG>
+// Y8: y is e4m3 with scales (else of x's type); RAG: rows that are no whole groups of 8
+template <typename T, int W, bool Y8, bool RAG>
 __global__ __launch_bounds__(W > 8 ? 64 * W : 512) void residual_norm_kernel(const NormArgs a)
 {
     constexpr int kWaves = W > 8 ? W : 8, kTeams = kWaves / W, kThreads = 64 * W;
@@ -101,104 +104,85 @@ __global__ __launch_bounds__(W > 8 ? 64 * W : 512) void residual_norm_kernel(con
     // (the same in all lanes of a wave: rows and their addresses are scalars)
     const int team = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / W, lane = threadIdx.x - team * kThreads;
     const float inv_cols = 1.0f / (float)a.cols;
-    int n[NC];  // elements of group k inside the row
-    float post[NC][8], pre[NC][8], gate[NC][8];
+    const Group<T, RAG> own(lane, kThreads, a.cols);
+    float post[8], pre[8], gate[8];
 #pragma unroll
-    for (int k = 0; k < NC; ++k) {
-        const int c = 8 * (k * kThreads + lane);
-        n[k] = a.cols - c;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) post[k][e] = pre[k][e] = gate[k][e] = 1.f;
-        if (a.post.p) a.post.template eight<RAG>(c, n[k], post[k]);
-        if (a.pre.p) a.pre.template eight<RAG>(c, n[k], pre[k]);
-    }
-    int64_t held = -1;  // the group of rows whose gate is in `gate`
-    const int64_t step = (int64_t)gridDim.x * kTeams;
-    Eight<T> u[NC], x[NC];
-    auto load = [&](int64_t r) {
-        r = min(r, a.rows - 1);
-#pragma unroll
-        for (int k = 0; k < NC; ++k) {
-            const int c = 8 * (k * kThreads + lane);
-            load_group<RAG>(u[k], (const T *)a.u + r * a.ldu, c, n[k]);
-            load_group<RAG>(x[k], (const T *)a.x + r * a.ldx, c, n[k]);
-        }
+    for (int e = 0; e < 8; ++e) post[e] = pre[e] = gate[e] = 1.f;
+    if (a.post.p) a.post.group(0, own, post);
+    if (a.pre.p) a.pre.group(0, own, pre);
+    int held = -1;  // the group of rows whose gate is in `gate`
+    const int step = gridDim.x * kTeams;
+    Eight<T> u, x;
+    auto load = [&](int to) {
+        const int64_t r = min(to, a.rows - 1);
+        own.load(u, (const T *)a.u + r * a.ldu);
+        own.load(x, (const T *)a.x + r * a.ldx);
     };
     // teams of a workgroup take neighbouring rows and run the same number of rounds: its barriers are met by all
-    int64_t row = (int64_t)blockIdx.x * kTeams + team;
-    load(row);
-    for (int64_t first = (int64_t)blockIdx.x * kTeams; first < a.rows; first += step, row += step) {
-        const bool live = row < a.rows;
+    int at = blockIdx.x * kTeams + team;
+    load(at);
+    for (int first = blockIdx.x * kTeams; first < a.rows; first += step, at += step) {
+        const int64_t row = at;
+        const bool live = at < a.rows;
         if (a.gate.p && live) {
-            const int64_t g = a.gate_rows == 1 ? row : row / a.gate_rows;
+            const int g = div_by(at, a.gate_rows, a.gate_magic);
             if (g != held) {
-#pragma unroll
-                for (int k = 0; k < NC; ++k) a.gate.template eight<RAG>(g * a.ldg + 8 * (k * kThreads + lane), n[k], gate[k]);
+                a.gate.group((int64_t)g * a.ldg, own, gate);
                 held = g;
             }
         }
-        float v[NC][8], h[NC][8], s = 0.f;
-#pragma unroll
-        for (int k = 0; k < NC; ++k) {
-            get_group(u[k], v[k], n[k] > 0);
-            get_group(x[k], h[k], n[k] > 0);
-        }
-        load(row + step);  // the next row's loads fly during this row's sums
+        float v[8], h[8], s = 0.f;
+        own.keep(u, true), own.keep(x, true);
+        u.get(v), x.get(h);
+        load(at + step);  // the next row's loads fly during this row's sums
         if (a.post.p) {
 #pragma unroll
-            for (int k = 0; k < NC; ++k)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) s = __builtin_fmaf(v[k][e], v[k][e], s);
+            for (int e = 0; e < 8; ++e) s = __builtin_fmaf(own.once(e, v[e]), v[e], s);
             s = team_sum<W>(s, red[0]);
             const float r1 = 1.0f / __builtin_sqrtf(s * inv_cols + a.eps);
             if (live && lane == 0 && a.r_post) a.r_post[row] = r1;
 #pragma unroll
-            for (int k = 0; k < NC; ++k)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[k][e] *= r1 * post[k][e];
+            for (int e = 0; e < 8; ++e) v[e] *= r1 * post[e];
         } else if (W > 1) {
             __syncthreads();  // the one sum's array is written again in the next round
         }
         s = 0.f;
 #pragma unroll
-        for (int k = 0; k < NC; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                h[k][e] = __builtin_fmaf(gate[k][e], v[k][e], a.residual_scale * h[k][e]);
-                s = __builtin_fmaf(h[k][e], h[k][e], s);
-            }
-        if (a.h && live) {
-#pragma unroll
-            for (int k = 0; k < NC; ++k) store_group<RAG>((T *)a.h + row * a.ldh, h[k], 8 * (k * kThreads + lane), n[k]);
+        for (int e = 0; e < 8; ++e) {
+            h[e] = __builtin_fmaf(gate[e], v[e], a.residual_scale * h[e]);
+            s = __builtin_fmaf(own.once(e, h[e]), h[e], s);
         }
+        if (a.h && live) own.store((T *)a.h + row * a.ldh, h);
         if (!a.y) {
-            if (W > 1) __syncthreads();  // the first sums' array is written again in the next round
+            if (W > 1) __syncthreads();  // as above
             continue;
         }
         s = team_sum<W>(s, red[1]);
         const float r2 = 1.0f / __builtin_sqrtf(s * inv_cols + a.eps);
         if (live && lane == 0 && a.r_pre) a.r_pre[row] = r2;
+        float y[8];
 #pragma unroll
-        for (int k = 0; k < NC; ++k) {
-            const int c = 8 * (k * kThreads + lane);
-            float y[8];
+        for (int e = 0; e < 8; ++e) y[e] = h[e] * r2 * pre[e];
+        if constexpr (!Y8) {
+            if (live) own.store((T *)a.y + row * a.ldy, y);
+        } else {
+            using F = Fp8<false>;
+            // a block is sixteen lanes' groups (bf16), or thirty-two lanes' halves of theirs (fp32)
+            float inv[8];
+            constexpr int kRun = Group<T, RAG>::kRun, kLanes = kBlock8 / kRun;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = h[k][e] * r2 * pre[k][e];
-            if constexpr (!Y8) {
-                if (live) store_group<RAG>((T *)a.y + row * a.ldy, y, c, n[k]);
-            } else {
-                using F = Fp8<false>;
+            for (int r = 0; r < 8; r += kRun) {
                 uint32_t m = 0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) m = max(m, n[k] > e ? magnitude(y[e]) : 0u);
-                const float q = F::scale(group_max_u32<16>(m)), inv = 1.0f / q;  // sixteen lanes hold a block
-                const uint32_t w[2] = {F::pack(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv),
-                                       F::pack(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv)};
-                if (live) {
-                    store_bytes<8>((uint8_t *)a.y + row * a.ldy + c, w, n[k]);
-                    if ((lane & 15) == 0 && n[k] > 0) a.y_scales[row * a.lds + c / kBlock8] = q;
-                }
+                for (int e = r; e < r + kRun; ++e) m = max(m, magnitude(own.in(e) ? own.once(e, y[e]) : 0.f));
+                const float q = F::scale(group_max_u32<kLanes>(m));
+#pragma unroll
+                for (int e = r; e < r + kRun; ++e) inv[e] = 1.0f / q;
+                if (live && lane % kLanes == 0 && own.in(r)) a.y_scales[row * a.lds + (lane + r / kRun * kThreads) / kLanes] = q;
             }
+            const uint32_t w[2] = {F::pack(y[0] * inv[0], y[1] * inv[1], y[2] * inv[2], y[3] * inv[3]),
+                                   F::pack(y[4] * inv[4], y[5] * inv[5], y[6] * inv[6], y[7] * inv[7])};
+            if (live) own.store_bytes((uint8_t *)a.y + row * a.ldy, w);
         }
     }
 }
@@ -210,9 +194,10 @@ __global__ __launch_bounds__(1024) void residual_norm_any_kernel(const NormArgs 
 {
     __shared__ float red[2][16];
     const float inv_cols = 1.0f / (float)a.cols;
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    for (int at = blockIdx.x; at < a.rows; at += gridDim.x) {
+        const int64_t row = at;
         const T *u = (const T *)a.u + row * a.ldu, *x = (const T *)a.x + row * a.ldx;
-        const int64_t g = a.gate.p ? row / a.gate_rows * a.ldg : 0;
+        const int64_t g = a.gate.p ? (int64_t)div_by(at, a.gate_rows, a.gate_magic) * a.ldg : 0;
         const int end = (a.cols + kBlock8 - 1) / kBlock8 * kBlock8;  // whole blocks: their lanes take part in the maximum
         float s = 0.f, r1 = 1.f;
         if (a.post.p) {
@@ -297,9 +282,10 @@ struct GradArgs {
     Param dgate;  // p is null where it is not asked for
     float *dpost, *dpre;
     float *ws;  // [2 runs][cols] sums of dgamma_pre and dgamma_post, then [2 runs][cols] of dgate
-    int64_t rows, lddy, lddh, ldh, ldu, ldg, gate_rows, lddx, lddu, lddg;
-    int64_t run;  // rows of a workgroup
-    int runs, cols;
+    int64_t lddy, lddh, ldh, ldu, ldg, lddx, lddu, lddg;
+    int rows, cols, gate_rows;
+    uint32_t gate_magic;
+    int run, runs;  // rows of a workgroup, and workgroups
     bool whole_groups;  // runs are whole groups of gate rows, and a team takes a group by itself
     float residual_scale;
 };
@@ -311,311 +297,243 @@ __device__ __forceinline__ float *gate_slot(const GradArgs &a, int64_t run, bool
     return a.ws + (2 * (int64_t)a.runs + 2 * run + (begins ? 1 : 0)) * a.cols;
 }
 
-// A row stays in registers as it came and is unpacked for each of its three uses; the gains and the gate lie in LDS, every
-// lane's own where it alone reads them (for rows of two groups per lane, which leave no room there, in the caches), and so do
-// two of the three sums of such rows.  With all of it in registers the kernel spilled 50 to 300 of them per lane.
-template <typename T, int W, int NC, bool RAG>
-__global__ __launch_bounds__(W > 8 ? 64 * W : 512, W <= 8 ? 2 : 4) void residual_norm_grad_kernel(const GradArgs a)
+// A row stays in registers as it came and is unpacked where it is used; gamma_pre, gate gamma_post and the sum that grows by
+// groups lie in LDS, every lane's own where it alone reads them: a lane has 128 registers.  Of the
+// three sums over rows two grow by the row, dy hn and H un: while the gate is the same, dgate is gamma_post times the latter
+// and dgamma_post the gate times it.
+template <typename T, int W, bool RAG>
+__global__ __launch_bounds__(1024) void residual_norm_grad_kernel(const GradArgs a)
 {
-    constexpr int kWaves = W > 8 ? W : 8, kTeams = kWaves / W, kThreads = 64 * W, kAll = 64 * kWaves;
-    constexpr bool kWide = NC > 1;
+    constexpr int kWaves = 16, kTeams = kWaves / W, kThreads = 64 * W, kAll = 64 * kWaves;
+    enum { kPre, kGatePost, kSumPost, kPlanes };
     __shared__ float red[2][kWaves];
-    __shared__ float joined[kTeams > 1 ? kAll * 8 : 1];
-    __shared__ float4_t own[kWide ? 2 : 3][2 * NC][kAll];  // gamma_post, gamma_pre, gate; of wide rows the sums of post and gate
+    __shared__ float4_t own[kPlanes][2][kAll];
     const int tid = threadIdx.x, team = __builtin_amdgcn_readfirstlane(tid >> 6) / W, lane = tid - team * kThreads;
     const float inv_cols = 1.0f / (float)a.cols;
     const bool has_post = a.post.p != nullptr, has_gate = a.gate.p != nullptr;
-    auto col = [&](int k) { return 8 * (k * kThreads + lane); };
-    auto get_own = [&](int which, int k, int q, float (&v)[4]) {
-        const float4_t f = own[which][2 * k + q][tid];
+    Group<T, RAG> here(lane, kThreads, a.cols);
+    auto get_own = [&](int which, int q, float (&v)[4]) {
+        const float4_t f = own[which][q][tid];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = f[e];
     };
-    auto put_own = [&](int which, int k, int q, const float (&v)[4]) { own[which][2 * k + q][tid] = float4_t{v[0], v[1], v[2], v[3]}; };
-    auto get_own8 = [&](int which, int k, float (&v)[8]) {
-        float lo[4], hi[4];
-        get_own(which, k, 0, lo), get_own(which, k, 1, hi);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = lo[e], v[4 + e] = hi[e];
+    auto put_own = [&](int which, const float (&v)[8]) {
+        own[which][0][tid] = float4_t{v[0], v[1], v[2], v[3]};
+        own[which][1][tid] = float4_t{v[4], v[5], v[6], v[7]};
     };
-    auto put_own8 = [&](int which, int k, const float (&v)[8]) {
-        const float lo[4] = {v[0], v[1], v[2], v[3]}, hi[4] = {v[4], v[5], v[6], v[7]};
-        put_own(which, k, 0, lo), put_own(which, k, 1, hi);
+    float sum_pre[8], sum_un[8], v8[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum_pre[e] = v8[e] = 0.f;
+    // gamma_post, or one, or the gate of group g, or one
+    auto get_post = [&](float (&v)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = 1.f;
+        if (has_post) a.post.group(0, here, v);
     };
-    int64_t g = 0;  // the group of rows whose gate is in use
-    auto param = [&](int which, int k, int q, float (&v)[4]) {
-        if constexpr (!kWide) {
-            get_own(which, k, q, v);
-        } else {
-            const Param &p = which == 0 ? a.post : which == 1 ? a.pre : a.gate;
-            const bool has = which == 0 ? has_post : which == 1 ? a.has_dy : has_gate;
+    auto get_gate = [&](int g, float (&v)[8]) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = 1.f;
-            if (has) p.four((which == 2 ? g * a.ldg : 0) + col(k) + 4 * q, a.cols - col(k) - 4 * q, v);
-        }
+        for (int e = 0; e < 8; ++e) v[e] = 1.f;
+        if (has_gate) a.gate.group((int64_t)g * a.ldg, here, v);
     };
-    float sum_pre[NC][8], sum_post[kWide ? 1 : NC][8], sum_gate[kWide ? 1 : NC][8];
-    const float zeros[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    auto clear_gate_sum = [&]() {
-#pragma unroll
-        for (int k = 0; k < NC; ++k) {
-            if constexpr (kWide) {
-                put_own8(1, k, zeros);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum_gate[k][e] = 0.f;
-            }
-        }
-    };
-#pragma unroll
-    for (int k = 0; k < NC; ++k) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum_pre[k][e] = 0.f;
-        if constexpr (kWide) {
-            put_own8(0, k, zeros);
-        } else {
-            float v[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = 1.f, sum_post[k][e] = 0.f;
-            put_own8(2, k, v);
-            if (has_post) a.post.template eight<RAG>(col(k), a.cols - col(k), v);
-            put_own8(0, k, v);
-            if (a.has_dy) a.pre.template eight<RAG>(col(k), a.cols - col(k), v);
-            put_own8(1, k, v);
-        }
-    }
+    const bool all_in = a.cols == 8 * kThreads && a.has_dy && a.has_dh;
 
-    Eight<T> dy[NC], dh[NC], h[NC], u[NC], next_dy[NC], next_dh[NC], next_h[NC], next_u[NC];
-    auto load = [&](int64_t r) {
-        r = min(r, a.rows - 1);
-#pragma unroll
-        for (int k = 0; k < NC; ++k) {
-            const int c = col(k), n = a.cols - c;
-            load_group<RAG>(next_dy[k], (const T *)a.dy + r * a.lddy, c, n);
-            load_group<RAG>(next_h[k], (const T *)a.h + r * a.ldh, c, n);
-            load_group<RAG>(next_dh[k], (const T *)a.dh + r * a.lddh, c, n);
-            load_group<RAG>(next_u[k], (const T *)a.u + r * a.ldu, c, n);
-        }
+    Eight<T> next_dy, next_dh, next_h, next_u;
+    float next_r2, next_r1;
+    auto load = [&](int to) {
+        const int64_t r = min(to, a.rows - 1);
+        // (a new value to the compiler for each row: it would keep a 64-bit address for every operand and lane otherwise)
+        asm volatile("" : "+v"(here.at[0]));
+        if constexpr (here.kRuns > 1) asm volatile("" : "+v"(here.at[1]));
+        here.load(next_dy, (const T *)a.dy + r * a.lddy);
+        here.load(next_h, (const T *)a.h + r * a.ldh);
+        here.load(next_dh, (const T *)a.dh + r * a.lddh);
+        here.load(next_u, (const T *)a.u + r * a.ldu);
+        // (not given: some other number, not used)
+        next_r2 = *(a.has_dy ? a.r_pre + r : a.ws), next_r1 = *(has_post ? a.r_post + r : a.ws);
     };
+    // Groups of few rows (whole_groups): a team takes every kTeams-th group by itself.  Otherwise the rows of the run that
+    // share a gate are dealt to the teams in turn.  Where all rows share it (spread), the rows are dealt to all teams of the
+    // chip instead, which then read one stretch of memory together (8192 x 4096: 90 us, with runs of neighbours 95).  All teams of a
+    // workgroup run the same number of rounds.
+    const int begin = blockIdx.x * a.run, end = min(a.rows, begin + a.run), per = a.gate_rows;
+    const bool each = a.whole_groups, spread = !each && per >= a.rows;
+    const int step = spread ? gridDim.x * kTeams : kTeams;
+    int g = div_by(begin, per, a.gate_magic) + (each ? team : 0);  // the group of rows whose gate is in use
+    int row = each ? g * per : (spread ? blockIdx.x * kTeams : begin) + team;
+    int from = begin;  // the round's first row, the same for all teams
+    load(row);  // (ahead of the parameters: both fly together)
+    put_own(kSumPost, v8);
+    if (a.has_dy) a.pre.group(0, here, v8);
+    put_own(kPre, v8);
+
     // one row of this team (a dead one adds nothing and writes nothing); `next` is loaded meanwhile
-    auto one = [&](int64_t row, bool live, int64_t next) {
-        const float r2 = a.has_dy && live ? a.r_pre[row] : 0.f, r1 = !has_post ? 1.f : live ? a.r_post[row] : 0.f;
-#pragma unroll
-        for (int k = 0; k < NC; ++k) {
-            const bool in = live && a.cols > col(k);
-            dy[k] = next_dy[k], h[k] = next_h[k], dh[k] = next_dh[k], u[k] = next_u[k];
-            dy[k].keep(in && a.has_dy), h[k].keep(in && a.has_dy), dh[k].keep(in && a.has_dh), u[k].keep(in);
+    auto one = [&](int64_t row, bool live, int next) {
+        const float r2 = a.has_dy && live ? next_r2 : 0.f, r1 = !has_post ? 1.f : live ? next_r1 : 0.f;
+        Eight<T> dy = next_dy, h = next_h, dh = next_dh, u = next_u;
+        if (!(live && all_in)) {
+            here.keep(dy, live && a.has_dy), here.keep(h, live && a.has_dy), here.keep(dh, live && a.has_dh), here.keep(u, live);
         }
         load(next);
         float s = 0.f;
         if (a.has_dy) {
 #pragma unroll
-            for (int k = 0; k < NC; ++k) {
+            for (int q = 0; q < 2; ++q) {
+                float t[4], hv[4], pre[4];
+                dy.get_half(q, t), h.get_half(q, hv), get_own(kPre, q, pre);
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    float t[4], hn[4], pre[4];
-                    dy[k].get_half(q, t), h[k].get_half(q, hn), param(1, k, q, pre);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        hn[e] *= r2;
-                        sum_pre[k][4 * q + e] = __builtin_fmaf(t[e], hn[e], sum_pre[k][4 * q + e]);
-                        s = __builtin_fmaf(t[e] * pre[e], hn[e], s);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);  // (reads of the next half's operands ahead of here cost registers)
+                for (int e = 0; e < 4; ++e) {
+                    const float th = t[e] * hv[e];
+                    sum_pre[4 * q + e] = __builtin_fmaf(th, r2, sum_pre[4 * q + e]);
+                    s = __builtin_fmaf(here.once(4 * q + e, th), pre[e], s);
                 }
+                __builtin_amdgcn_sched_barrier(0);  // (reads of the next half's operands ahead of here cost registers)
             }
             s = team_sum<W>(s, red[0]);
         } else if (W > 1) {
             __syncthreads();  // the one sum's array is written again in the next row
         }
-        const float mean2 = s * inv_cols;
-        auto into_h = [&](int k, int q, float (&H)[4]) {
-            float t[4], hn[4], pre[4];
-            dy[k].get_half(q, t), h[k].get_half(q, hn), dh[k].get_half(q, H), param(1, k, q, pre);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) H[e] = __builtin_fmaf(r2, t[e] * pre[e] - hn[e] * r2 * mean2, H[e]);
-        };
-        auto renew = [&]() {
-#pragma unroll
-            for (int k = 0; k < NC; ++k) dy[k].renew(), h[k].renew(), dh[k].renew(), u[k].renew();
-        };
-        renew();
+        const float of_h = -r2 * r2 * (r2 * s * inv_cols);  // H = dh + r2 t - r2 hn mean(t hn)
+        dy.renew(), h.renew();
         s = 0.f;
+        float v[8], dx[8];
 #pragma unroll
-        for (int k = 0; k < NC; ++k) {
-            float dx[8];
+        for (int q = 0; q < 2; ++q) {
+            float t[4], hv[4], H[4], pre[4], un[4], gp[4];
+            dy.get_half(q, t), h.get_half(q, hv), dh.get_half(q, H), u.get_half(q, un);
+            get_own(kPre, q, pre), get_own(kGatePost, q, gp);
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                float H[4], un[4], post[4], gate[4], more_post[4], more_gate[4];
-                into_h(k, q, H);
-                u[k].get_half(q, un), param(0, k, q, post), param(2, k, q, gate);
-                if constexpr (kWide) get_own(0, k, q, more_post), get_own(1, k, q, more_gate);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    un[e] *= r1;
-                    const float d = H[e] * gate[e];
-                    float &to_post = kWide ? more_post[e] : sum_post[kWide ? 0 : k][4 * q + e];
-                    float &to_gate = kWide ? more_gate[e] : sum_gate[kWide ? 0 : k][4 * q + e];
-                    to_post = __builtin_fmaf(d, un[e], to_post);
-                    to_gate = __builtin_fmaf(un[e] * post[e], H[e], to_gate);
-                    s = __builtin_fmaf(d * post[e], un[e], s);
-                    dx[4 * q + e] = a.residual_scale * H[e];
-                }
-                if constexpr (kWide) put_own(0, k, q, more_post), put_own(1, k, q, more_gate);
-                __builtin_amdgcn_sched_barrier(0);
+            for (int e = 0; e < 4; ++e) {
+                H[e] = __builtin_fmaf(hv[e], of_h, __builtin_fmaf(t[e] * pre[e], r2, H[e]));
+                un[e] *= r1;
+                sum_un[4 * q + e] = __builtin_fmaf(H[e], un[e], sum_un[4 * q + e]);
+                v[4 * q + e] = H[e] * gp[e];
+                s = __builtin_fmaf(here.once(4 * q + e, v[4 * q + e]), un[e], s);
+                dx[4 * q + e] = a.residual_scale * H[e];
             }
-            if (live) store_group<RAG>((T *)a.dx + row * a.lddx, dx, col(k), a.cols - col(k));
+            __builtin_amdgcn_sched_barrier(0);
         }
-        float mean1 = 0.f;
-        if (has_post)
-            mean1 = team_sum<W>(s, red[1]) * inv_cols;
-        else if (W > 1)
+        if (live) here.store((T *)a.dx + row * a.lddx, dx);
+        if (has_post) {
+            const float of_u = -r1 * r1 * (team_sum<W>(s, red[1]) * inv_cols);  // du = r1 v - r1 un mean(v un)
+            u.renew();
+            float uv[8];
+            u.get(uv);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(uv[e], of_u, r1 * v[e]);
+        } else if (W > 1) {
             __syncthreads();  // as above
-        renew();
-#pragma unroll
-        for (int k = 0; k < NC; ++k) {
-            float du[8];
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                float H[4], un[4], post[4], gate[4];
-                into_h(k, q, H);
-                u[k].get_half(q, un), param(0, k, q, post), param(2, k, q, gate);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) du[4 * q + e] = r1 * (H[e] * gate[e] * post[e] - un[e] * r1 * mean1);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            if (live) store_group<RAG>((T *)a.du + row * a.lddu, du, col(k), a.cols - col(k));
         }
+        if (live) here.store((T *)a.du + row * a.lddu, v);
     };
-    // the teams' sums v, added in the teams' order; the first team has them
+    // the teams' sums v, added in the teams' order: the first team has them.  The gate's place serves, until the next one comes
     auto join = [&](float (&v)[8]) {
         if constexpr (kTeams > 1) {
-            static_assert(NC == 1, "teams of fewer than eight waves hold one group per lane");
             __syncthreads();
-#pragma unroll
-            for (int e = 0; e < 8; ++e) joined[e * kAll + tid] = v[e];
+            put_own(kGatePost, v);
             __syncthreads();
             if (team == 0) {
                 for (int o = 1; o < kTeams; ++o)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] += joined[e * kAll + o * kThreads + lane];
+                    for (int e = 0; e < 8; ++e) v[e] += own[kGatePost][e >> 2][o * kThreads + lane][e & 3];
             }
+            __syncthreads();
         }
     };
 
-    // Groups of few rows (whole_groups): a team takes every kTeams-th group by itself.  Otherwise the rows of the run that
-    // share a gate are dealt to the teams in turn.  All teams run the same number of rounds.
-    const int64_t begin = (int64_t)blockIdx.x * a.run, end = min(a.rows, begin + a.run);
-    const int64_t per = has_gate ? a.gate_rows : a.rows;
-    const bool each = a.whole_groups;
-    g = begin / per + (each ? team : 0);
-    int64_t row = each ? g * per : begin + team;
-    int64_t from = begin;  // the round's first row, the same for all teams
-    load(row);
     while (from < end) {
-        const int64_t stop = min(end, (g + 1) * per);
-        if constexpr (!kWide) {
-            if (has_gate && g * per < end) {
+        const int stop = spread ? a.rows : min(end, (g + 1) * per), first = spread ? blockIdx.x * kTeams : from;
+        if (g * per < end) {
+            float gate[8];
+            get_gate(g, gate), get_post(v8);
 #pragma unroll
-                for (int k = 0; k < NC; ++k) {
-                    float v[8];
-                    a.gate.template eight<RAG>(g * a.ldg + col(k), a.cols - col(k), v);
-                    put_own8(2, k, v);
-                }
-            }
+            for (int e = 0; e < 8; ++e) v8[e] *= gate[e];
+            put_own(kGatePost, v8);
         }
-        clear_gate_sum();
-        const int64_t rounds = each ? per : (stop - from + kTeams - 1) / kTeams;
-        for (int64_t i = rounds; i > 0; --i) {
-            const int64_t next = each ? (i > 1 ? row + 1 : (g + kTeams) * per) : (i > 1 ? row + kTeams : stop + team);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum_un[e] = 0.f;
+        const int rounds = each ? per : (stop - first + step - 1) / step;
+        for (int i = rounds; i > 0; --i) {
+            const int next = each ? (i > 1 ? row + 1 : (g + kTeams) * per) : (i > 1 ? row + step : stop + team);
             one(row, row < stop, next);
             row = next;
         }
+if (a.dpost && g * per < end) {
+            float lo[4], hi[4];
+            get_gate(g, v8), get_own(kSumPost, 0, lo), get_own(kSumPost, 1, hi);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v8[e] = __builtin_fmaf(v8[e], sum_un[e], e < 4 ? lo[e & 3] : hi[e & 3]);
+            put_own(kSumPost, v8);
+        }
         if (a.dgate.p) {
+            if (!each) join(sum_un);
             const bool begins = g * per >= begin, ends = min(a.rows, (g + 1) * per) <= end;
+            if (each ? g * per < end : team == 0) {
+                get_post(v8);
 #pragma unroll
-            for (int k = 0; k < NC; ++k) {
-                float v[8];
-                if constexpr (kWide)
-                    get_own8(1, k, v);
+                for (int e = 0; e < 8; ++e) sum_un[e] *= v8[e];
+                if (begins && ends)
+                    a.dgate.put_group((int64_t)g * a.lddg, here, sum_un);
                 else
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = sum_gate[k][e];
-                if (!each) join(v);
-                if (each ? g * per < end : team == 0) {
-                    if (begins && ends)
-                        a.dgate.template put_eight<RAG>(g * a.lddg, v, col(k), a.cols - col(k));
-                    else
-                        store_group<RAG>(gate_slot(a, blockIdx.x, begins), v, col(k), a.cols - col(k));
-                }
+                    here.store(gate_slot(a, blockIdx.x, begins), sum_un);
             }
         }
         g += each ? kTeams : 1;
         from = each ? (g - team) * per : stop;
     }
+    if (a.dpre && a.has_dy) {
+        join(sum_pre);
+        if (team == 0) here.store(a.ws + (int64_t)blockIdx.x * a.cols, sum_pre);
+    }
+    if (a.dpost) {
+        float lo[4], hi[4];
+        get_own(kSumPost, 0, lo), get_own(kSumPost, 1, hi);
 #pragma unroll
-    for (int k = 0; k < NC; ++k) {
-        if (a.dpre && a.has_dy) {
-            join(sum_pre[k]);
-            if (team == 0) store_group<RAG>(a.ws + (int64_t)blockIdx.x * a.cols, sum_pre[k], col(k), a.cols - col(k));
-        }
-        if (a.dpost) {
-            float v[8];
-            if constexpr (kWide)
-                get_own8(0, k, v);
-            else
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = sum_post[k][e];
-            join(v);
-            if (team == 0) store_group<RAG>(a.ws + ((int64_t)a.runs + blockIdx.x) * a.cols, v, col(k), a.cols - col(k));
-        }
+        for (int e = 0; e < 4; ++e) v8[e] = lo[e], v8[4 + e] = hi[e];
+        join(v8);
+        if (team == 0) here.store(a.ws + ((int64_t)a.runs + blockIdx.x) * a.cols, v8);
     }
 }
 
-// The runs' sums, added in the order of the rows.  blockIdx.y: 0 = dgamma_pre, 1 = dgamma_post, 2 + t = the gate of the group
-// that begins in run t and goes on beyond it.  64 columns and four parts of the runs per workgroup, the parts added in order.
-__global__ __launch_bounds__(256) void residual_norm_sums_kernel(const GradArgs a)
+// The runs' sums, added in the order of the rows.  blockIdx.y: 0 = dgamma_pre, 1 = dgamma_post, then the gates of groups that
+// begin in one run and go on beyond it: by group, or (by_run) by the run in which it begins, whichever are fewer.  64 columns
+// and sixteen parts of the runs per workgroup, the parts added in order.
+__global__ __launch_bounds__(1024) void residual_norm_sums_kernel(const GradArgs a, bool by_run)
 {
-    const int64_t col = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
-    const int part = threadIdx.x >> 6, which = blockIdx.y;
-    const float *from;
-    int64_t count, step = a.cols, g = 0;
-    __shared__ float parts[3][64];
-    const bool in = col < a.cols;
+    constexpr int kParts = 16;
+    __shared__ float parts[kParts][64];
+    const int lane = threadIdx.x & 63, part = threadIdx.x >> 6, col = blockIdx.x * 64 + lane;
+    const int which = blockIdx.y;
+    int count = a.runs, g = 0;
+    const float *from = a.ws + (int64_t)which * a.runs * a.cols;  // the sums of run i lie `step` after those of run i - 1
+    int64_t step = a.cols;
     if (which < 2) {
-        float *to = which ? a.dpost : a.dpre;
-        if (!to) return;
-        from = a.ws + (int64_t)which * a.runs * a.cols;
-        count = which == 0 && !a.has_dy ? 0 : a.runs;
+        if (!(which ? a.dpost : a.dpre)) return;
+        if (which == 0 && !a.has_dy) count = 0;
     } else {
-        const int64_t t = which - 2, last = min(a.rows, (t + 1) * a.run) - 1;
-        g = last / a.gate_rows;
-        const int64_t begin = g * a.gate_rows, end = min(a.rows, begin + a.gate_rows);
-        if (begin < t * a.run || end <= last + 1) return;
-        from = nullptr;
+        g = by_run ? div_by(min(a.rows, (which - 1) * a.run) - 1, a.gate_rows, a.gate_magic) : which - 2;
+        const int begin = g * a.gate_rows, end = min(a.rows, begin + a.gate_rows), t = begin / a.run;
+        if ((by_run && t != which - 2) || end <= (t + 1) * a.run) return;
+        from = gate_slot(a, t, true);  // ... of the first, one row of slots early for the others
+        step = 2 * (int64_t)a.cols;
         count = (end - 1) / a.run - t + 1;
     }
-    const int64_t per = (count + 3) / 4, lo = part * per, hi = min(count, lo + per);
+    const int per = (count + kParts - 1) / kParts, lo = part * per, hi = min(count, lo + per);
     float s = 0.f;
-    if (in) {
-        if (from) {
+    if (col < a.cols) {
 #pragma unroll 8
-            for (int64_t i = lo; i < hi; ++i) s += from[i * step + col];
-        } else {
-            const int64_t t = which - 2;
-            for (int64_t i = lo; i < hi; ++i) s += gate_slot(a, t + i, i == 0)[col];
-        }
+        for (int i = lo; i < hi; ++i) s += from[i * step - (which >= 2 && i > 0 ? a.cols : 0) + col];
     }
-    if (part) parts[part - 1][threadIdx.x & 63] = s;
+    parts[part][lane] = s;
     __syncthreads();
-    if (part || !in) return;
-    s = ((s + parts[0][threadIdx.x]) + parts[1][threadIdx.x]) + parts[2][threadIdx.x];
+    if (part || col >= a.cols) return;
+#pragma unroll
+    for (int p = 1; p < kParts; ++p) s += parts[p][lane];
     if (which == 0)
         a.dpre[col] = s;
     else if (which == 1)
         a.dpost[col] = s;
     else
-        a.dgate.put(g * a.lddg + col, s);
+        a.dgate.put((int64_t)g * a.lddg + col, s);
 }
 
 // Rows of any length, in three kernels: every row's mean(t hn) into the workspace; a lane per column, which computes H
@@ -635,9 +553,10 @@ __global__ __launch_bounds__(1024) void residual_norm_grad_any_kernel(const Grad
 {
     __shared__ float red[1][16];
     const float inv_cols = 1.0f / (float)a.cols;
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    for (int at = blockIdx.x; at < a.rows; at += gridDim.x) {
+        const int64_t row = at;
         const float r2 = a.has_dy ? a.r_pre[row] : 0.f, r1 = a.post.p ? a.r_post[row] : 1.f;
-        const int64_t g = a.gate.p ? row / a.gate_rows * a.ldg : 0;
+        const int64_t g = a.gate.p ? (int64_t)div_by(at, a.gate_rows, a.gate_magic) * a.ldg : 0;
         float s = 0.f;
         if constexpr (MEANS) {
             if (a.has_dy) {
@@ -674,13 +593,12 @@ __global__ __launch_bounds__(256) void residual_norm_grad_cols_kernel(const Grad
 {
     const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (c >= a.cols) return;
-    const int64_t begin = (int64_t)blockIdx.y * a.run, end = min(a.rows, begin + a.run);
-    const int64_t per = a.gate.p ? a.gate_rows : a.rows;
+    const int begin = blockIdx.y * a.run, end = min(a.rows, begin + a.run), per = a.gate_rows;
     const float post = a.post.p ? a.post.at(c) : 1.f;
     float sum_pre = 0.f, sum_post = 0.f;
-    for (int64_t from = begin; from < end;) {
-        const int64_t g = from / per, to = min(end, (g + 1) * per);
-        const float gate = a.gate.p ? a.gate.at(g * a.ldg + c) : 1.f;
+    for (int from = begin; from < end;) {
+        const int g = div_by(from, per, a.gate_magic), to = min(end, (g + 1) * per);
+        const float gate = a.gate.p ? a.gate.at((int64_t)g * a.ldg + c) : 1.f;
         float sum_gate = 0.f;
         for (int64_t row = from; row < to; ++row) {
             const float r2 = a.has_dy ? a.r_pre[row] : 0.f, r1 = a.post.p ? a.r_post[row] : 1.f;
@@ -695,7 +613,7 @@ __global__ __launch_bounds__(256) void residual_norm_grad_cols_kernel(const Grad
         if (a.dgate.p) {
             const bool begins = g * per >= begin, ends = min(a.rows, (g + 1) * per) <= end;
             if (begins && ends)
-                a.dgate.put(g * a.lddg + c, sum_gate);
+                a.dgate.put((int64_t)g * a.lddg + c, sum_gate);
             else
                 gate_slot(a, blockIdx.y, begins)[c] = sum_gate;
         }
@@ -706,83 +624,89 @@ __global__ __launch_bounds__(256) void residual_norm_grad_cols_kernel(const Grad
 }
 
 // ---- entry points --------------------------------------------------------------------------------------------------
-constexpr int kWidest = 16 * 64 * 8;  // columns that a team of 16 waves holds
+// columns of the kernels that hold a row: a group of eight, and what 16 waves have room for
+constexpr int kNarrowest = 8, kWidest = 16 * 64 * 8;
+inline bool row_fits(int64_t cols) { return cols >= kNarrowest && cols <= kWidest; }
 
-// f(waves of a team, groups per lane) for rows of `cols` elements within kWidest
+// f(waves of a team) for rows that fit one
 template <typename F>
 static void with_team(int64_t cols, F &&f)
 {
     using std::integral_constant;
     if (cols <= 512)
-        f(integral_constant<int, 1>{}, integral_constant<int, 1>{});
+        f(integral_constant<int, 1>{});
     else if (cols <= 1024)
-        f(integral_constant<int, 2>{}, integral_constant<int, 1>{});
+        f(integral_constant<int, 2>{});
     else if (cols <= 2048)
-        f(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+        f(integral_constant<int, 4>{});
     else if (cols <= 4096)
-        f(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+        f(integral_constant<int, 8>{});
     else
-        f(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+        f(integral_constant<int, 16>{});
 }
 
 template <typename T, bool Y8>
 static void launch_norm(const NormArgs &a, hipStream_t stream)
 {
-    if (a.cols > kWidest) {
+    if (!row_fits(a.cols)) {
         residual_norm_any_kernel<T, Y8><<<(unsigned)std::min<int64_t>(a.rows, 65536), 1024, 0, stream>>>(a);
         return;
     }
-    with_team(a.cols, [&](auto w, auto nc) {
-        constexpr int W = w, NC = nc, kTeams = W > 8 ? 1 : 8 / W, kThreads = W > 8 ? 1024 : 512;
-        const int64_t grid = std::min<int64_t>((a.rows + kTeams - 1) / kTeams, 1024 * 512 / kThreads);
+    with_team(a.cols, [&](auto w) {
+        constexpr int W = w, kTeams = W > 8 ? 1 : 8 / W, kThreads = W > 8 ? 1024 : 512;
+        // One workgroup per CU: more of them read more places of memory at once (8192 x 4096 bf16: 46.7 us with 256, 48.5 with
+        // 512, 53 with 1024).  A gate that changes after a few rows is waited for, which a second one hides (of every element's
+        // own: 56 us with 512, 79 with 256).
+        const int64_t most = a.gate.p && a.gate_rows < 16 ? 512 : 256;
+        const int64_t grid = std::min<int64_t>((a.rows + kTeams - 1) / kTeams, most);
         if (a.cols % 8)
-            residual_norm_kernel<T, W, NC, Y8, true><<<(unsigned)grid, kThreads, 0, stream>>>(a);
+            residual_norm_kernel<T, W, Y8, true><<<(unsigned)grid, kThreads, 0, stream>>>(a);
         else
-            residual_norm_kernel<T, W, NC, Y8, false><<<(unsigned)grid, kThreads, 0, stream>>>(a);
+            residual_norm_kernel<T, W, Y8, false><<<(unsigned)grid, kThreads, 0, stream>>>(a);
     });
 }
 
 // Rows of a workgroup's run in the gradient, and whether the runs are whole groups of a gate.
 struct RunPlan {
-    int64_t run;
-    int runs;
+    int run, runs;
     bool whole_groups;
 };
+// A run for each CU.
 static RunPlan plan_runs(int64_t rows, int64_t cols, int64_t gate_rows)
 {
-    const int64_t teams = cols <= 512 ? 8 : cols <= 1024 ? 4 : cols <= 2048 ? 2 : 1;
-    const int64_t most = cols <= 4096 ? 512 : 256;
+    const int64_t teams = cols <= 512 ? 16 : cols <= 1024 ? 8 : cols <= 2048 ? 4 : cols <= 4096 ? 2 : 1, most = 256;
     RunPlan p;
     p.whole_groups = gate_rows <= 16;
     const int64_t unit = teams * (p.whole_groups ? gate_rows : 1);
-    p.run = ((rows + most - 1) / most + unit - 1) / unit * unit;
+    p.run = (int)(((rows + most - 1) / most + unit - 1) / unit * unit);
     p.runs = (int)((rows + p.run - 1) / p.run);
     return p;
 }
-static int64_t gate_rows_or_all(int64_t gate_rows, int64_t rows) { return gate_rows < 1 || gate_rows > rows ? rows : gate_rows; }
 
 template <typename T>
 static void launch_grad(GradArgs a, hipStream_t stream)
 {
-    if (a.cols > kWidest) {
+    if (!row_fits(a.cols)) {
         float *means = a.ws + 4 * (int64_t)a.runs * a.cols;
         const unsigned grid = (unsigned)std::min<int64_t>(a.rows, 65536);
         residual_norm_grad_any_kernel<T, true><<<grid, 1024, 0, stream>>>(a, means);
         residual_norm_grad_cols_kernel<T><<<dim3((a.cols + 255) / 256, a.runs), 256, 0, stream>>>(a, means);
         residual_norm_grad_any_kernel<T, false><<<grid, 1024, 0, stream>>>(a, means);
     } else {
-        with_team(a.cols, [&](auto w, auto nc) {
-            constexpr int W = w, NC = nc;
+        with_team(a.cols, [&](auto w) {
+            constexpr int W = w;
             if (a.cols % 8)
-                residual_norm_grad_kernel<T, W, NC, true><<<a.runs, W > 8 ? 1024 : 512, 0, stream>>>(a);
+                residual_norm_grad_kernel<T, W, true><<<a.runs, 1024, 0, stream>>>(a);
             else
-                residual_norm_grad_kernel<T, W, NC, false><<<a.runs, W > 8 ? 1024 : 512, 0, stream>>>(a);
+                residual_norm_grad_kernel<T, W, false><<<a.runs, 1024, 0, stream>>>(a);
         });
     }
-    const unsigned blocks = (unsigned)((a.cols + 63) / 64);
     // (a gate whose groups lie within runs has its sums already)
-    const unsigned gates = a.dgate.p && !(a.cols <= kWidest && a.whole_groups) ? a.runs : 0;
-    if (a.dpre || a.dpost || gates) residual_norm_sums_kernel<<<dim3(blocks, 2 + gates), 256, 0, stream>>>(a);
+    const int groups = (a.rows + a.gate_rows - 1) / a.gate_rows;
+    const bool by_run = groups > a.runs;
+    const int gates = a.dgate.p && !a.whole_groups ? std::min(groups, a.runs) : 0;
+    if (a.dpre || a.dpost || gates)
+        residual_norm_sums_kernel<<<dim3((a.cols + 63) / 64, 2 + gates), 1024, 0, stream>>>(a, by_run);
 }
 
 }  // namespace perf
@@ -796,7 +720,7 @@ extern "C" perf_status perf_residual_norm(const void *u, const void *x, const vo
     using namespace perf;
     const bool y8 = y && y_dt == PERF_E4M3;
     if (!u || !x || (!h && !y) || (y && !gamma_pre) || (y8 && !y_scales)) return PERF_ERR_NULL;
-    if (rows < 1 || cols < 1 || cols > kMaxExtent8 || ldu < cols || ldx < cols || (h && ldh < cols) || (y && ldy < cols))
+    if (rows < 1 || cols < 1 || rows > kMaxExtent8 || cols > kMaxExtent8 || ldu < cols || ldx < cols || (h && ldh < cols) || (y && ldy < cols))
         return PERF_ERR_SHAPE;
     if (gate && (ldg < cols || gate_rows < 1)) return PERF_ERR_SHAPE;
     if (y8 && lds < (cols + kBlock8 - 1) / kBlock8) return PERF_ERR_SHAPE;
@@ -809,10 +733,9 @@ extern "C" perf_status perf_residual_norm(const void *u, const void *x, const vo
         (y8 && !aligned(y_scales, 4)))
         return PERF_ERR_ALIGN;
     if (y && !y8 && y_dt != x_dt) return PERF_ERR_UNSUPPORTED;
-    const int pb = param_dt == PERF_BF16;
+    const int pb = param_dt == PERF_BF16, per = (int)(gate ? std::min(gate_rows, rows) : rows);
     const NormArgs a{u, x, Param{gate, gate_dt == PERF_BF16}, Param{gamma_post, pb}, Param{y ? gamma_pre : nullptr, pb}, h, y, y_scales,
-                     rrms_post, rrms_pre, rows, ldu, ldx, ldg, gate ? gate_rows_or_all(gate_rows, rows) : rows, ldh, ldy, lds,
-                     (int)cols, residual_scale, eps};
+                     rrms_post, rrms_pre, ldu, ldx, ldg, ldh, ldy, lds, (int)rows, (int)cols, per, div_magic(per), residual_scale, eps};
     const hipStream_t st = (hipStream_t)stream;
     if (x_dt == PERF_BF16) {
         if (y8)
@@ -831,10 +754,10 @@ extern "C" perf_status perf_residual_norm(const void *u, const void *x, const vo
 extern "C" int64_t perf_residual_norm_backward_workspace_bytes(int64_t rows, int64_t cols)
 {
     using namespace perf;
-    if (rows < 1 || cols < 1 || cols > kMaxExtent8) return -1;
-    // (runs of whole groups are longer, so there are no more of them)
+    if (rows < 1 || cols < 1 || rows > kMaxExtent8 || cols > kMaxExtent8) return -1;
+    // (runs of whole groups are longer: there are no more of them)
     const RunPlan p = plan_runs(rows, cols, INT64_MAX);
-    return 4 * (4 * (int64_t)p.runs * cols + (cols > kWidest ? rows : 0));
+    return 4 * (4 * (int64_t)p.runs * cols + (row_fits(cols) ? 0 : rows));
 }
 
 extern "C" perf_status perf_residual_norm_backward(const void *dy, const void *dh, const void *h, const void *u, const void *gate,
@@ -849,7 +772,7 @@ extern "C" perf_status perf_residual_norm_backward(const void *dy, const void *d
     if ((!dy && !dh) || !u || !dx || !du || !workspace) return PERF_ERR_NULL;
     if (dy && (!h || !gamma_pre || !rrms_pre)) return PERF_ERR_NULL;
     if ((gamma_post && !rrms_post) || (dgate && !gate) || (dgamma_post && !gamma_post) || (dgamma_pre && !dy)) return PERF_ERR_NULL;
-    if (rows < 1 || cols < 1 || cols > kMaxExtent8 || (dy && (lddy < cols || ldh < cols)) || (dh && lddh < cols) || ldu < cols ||
+    if (rows < 1 || cols < 1 || rows > kMaxExtent8 || cols > kMaxExtent8 || (dy && (lddy < cols || ldh < cols)) || (dh && lddh < cols) || ldu < cols ||
         lddx < cols || lddu < cols)
         return PERF_ERR_SHAPE;
     if (gate && (ldg < cols || gate_rows < 1 || (dgate && lddg < cols))) return PERF_ERR_SHAPE;
@@ -862,12 +785,12 @@ extern "C" perf_status perf_residual_norm_backward(const void *dy, const void *d
         !aligned(dgamma_pre, 4) || !aligned(workspace, 4))
         return PERF_ERR_ALIGN;
     const int pb = param_dt == PERF_BF16, gb = gate_dt == PERF_BF16;
-    const int64_t per = gate ? gate_rows_or_all(gate_rows, rows) : rows;
+    const int per = (int)(gate ? std::min(gate_rows, rows) : rows);
     const RunPlan p = plan_runs(rows, cols, per);
     GradArgs a{dy ? dy : u, dh ? dh : u, dy ? h : u, u, dy != nullptr, dh != nullptr, Param{gate, gb}, Param{gamma_post, pb},
-               Param{gamma_pre, pb}, rrms_post, rrms_pre, dx, du, Param{dgate, gb}, dgamma_post, dgamma_pre, (float *)workspace, rows,
-               dy ? lddy : ldu, dh ? lddh : ldu, dy ? ldh : ldu, ldu, ldg, per, lddx, lddu, lddg, p.run, p.runs, (int)cols,
-               gate && p.whole_groups, residual_scale};
+               Param{gamma_pre, pb}, rrms_post, rrms_pre, dx, du, Param{dgate, gb}, dgamma_post, dgamma_pre, (float *)workspace,
+               dy ? lddy : ldu, dh ? lddh : ldu, dy ? ldh : ldu, ldu, ldg, lddx, lddu, lddg, (int)rows, (int)cols, per, div_magic(per),
+               p.run, p.runs, gate && p.whole_groups, residual_scale};
     if (x_dt == PERF_BF16)
         launch_grad<uint16_t>(a, (hipStream_t)stream);
     else
