@@ -13,6 +13,7 @@
 //  * gemm_fp8_tile_kernel: operands pass through LDS, two stages of one block of K; a workgroup tile of 256 x 256 or less.
 //  * gemm_fp8_waves_kernel: few output tiles or few rows; the waves of a workgroup share one tile and divide the blocks
 //    of K; operands go straight to registers, and the waves' sums are added through LDS in the waves' order.
+#include <atomic>
 #include "fp8.h"
 #include "mfma_tile.h"
 #include "host_utils.h"
@@ -62,16 +63,16 @@ __device__ __forceinline__ Fragment<WIDE> as_fragment(int8v_t v)
     return f;
 }
 
-// 16 x 16 sums of a block: rows of B (e4m3) by rows of A (e4m3, or e5m2 with A5)
+// 16 x 16 sums of a block: rows of B (e4m3) by rows of A (e4m3, or e5m2 with A5), times 2^(exponent - 127)
 template <bool WIDE, bool A5>
-__device__ __forceinline__ float4_t mma_block(const Fragment<WIDE> &b, const Fragment<WIDE> &a)
+__device__ __forceinline__ float4_t mma_block(const Fragment<WIDE> &b, const Fragment<WIDE> &a, int exponent = 127)
 {
     float4_t c = {0.f, 0.f, 0.f, 0.f};
     if constexpr (WIDE) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.v[q], a.v[q], c, 0, 0, 0);
     } else {
-        c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b.v, a.v, c, 0, A5 ? 1 : 0, 0, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b.v, a.v, c, 0, A5 ? 1 : 0, 0, exponent, 0, 127);
     }
     return c;
 }
@@ -89,9 +90,13 @@ __device__ __forceinline__ int4v_t keep_first(int4v_t v, int n)
 
 // An operand's rows as a buffer that ends with the last row's last element, rounded up to whole words (a word that holds an
 // element is readable): what lies behind reads as zero.  Rows of a tile past the matrix read its last row instead.
+__device__ __forceinline__ uint32_t operand_bytes(int rows, int64_t ld, int K)
+{
+    return (uint32_t)(((int64_t)(rows - 1) * ld + K + 3) & ~(int64_t)3);
+}
 __device__ __forceinline__ rsrc_t operand_rsrc(const uint8_t *base, int rows, int64_t ld, int K)
 {
-    return make_rsrc(base, (uint32_t)(((int64_t)(rows - 1) * ld + K + 3) & ~(int64_t)3));
+    return make_rsrc(base, operand_bytes(rows, ld, K));
 }
 
 // A lane's 32 elements of a row in a block: the 16 from 16 * (lane / 16) on, and those 64 further on.  `left`: elements of
@@ -141,7 +146,8 @@ __global__ __launch_bounds__(64 * W) void gemm_fp8_waves_kernel(const Gemm8Args 
     constexpr bool WIDE = sizeof(CT) == 4;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t bz = blockIdx.y;
-    const int tile_m = (int)blockIdx.x % tiles_m, tile_n = (int)blockIdx.x / tiles_m;
+    // (divisions leave vector registers)
+    const int tile_n = __builtin_amdgcn_readfirstlane((int)blockIdx.x / tiles_m), tile_m = (int)blockIdx.x - tile_n * tiles_m;
     const int m0 = tile_m * 16 * TM, n0 = tile_n * 16 * TN;
     const int rows_m = min(16 * TM, g.M - m0), rows_n = min(16 * TN, g.N - n0);
     const int blocks = (g.K + kBlock8 - 1) / kBlock8;
@@ -218,126 +224,298 @@ __global__ __launch_bounds__(64 * W) void gemm_fp8_waves_kernel(const Gemm8Args 
     }
 }
 
+constexpr int kScaleStage = 2048;  // bytes of LDS for the scales of a block: one for each row of a tile of A and of B, or for 128 of B
+
+// All of this wave's LDS accesses are done; its loads stay in flight.
+__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xC07F); }
+
 // WM x WN waves, each with TM x TN groups of 16 rows of A and of B.  LDS: two stages of a block of K, rows of 128 bytes whose
-// 16-byte chunks are permuted as in mfma_tile.h (swz64), and the block's scales.  A step waits for its stage, which had the
-// whole step before to arrive, starts the loads of the next, and multiplies: B's fragments stay in registers, A's pass by.
+// 16-byte chunks are permuted as in mfma_tile.h (swz64), and the block's scales.
+//
+// A step multiplies a block: B's fragments stay in registers, A's pass by, up to four groups ahead; a sum is scaled and
+// added behind the third product after its own (a sum can be used some 50 cycles after its instruction; behind the fourth it
+// is no faster and takes 16 more registers, in front of that product a lone wave needs 37 cycles for each and not 33).  The waves
+// meet once, before the last of these groups, whose fragments are in registers by then: the next stage has arrived, this one is
+// free.  Its reload is spread over those groups: in a burst the loads fill the texture path, and a wave whose load cannot
+// issue holds back the products behind it.
+//
+// The scale of a 128 x 128 tile of B (B128) is the same for all sums of a wave: its exponent goes into the matrix
+// instruction, its mantissa into the factor of A's scale, which leaves one multiply-add per sum, and no product of two
+// scales that could leave fp32's range.
 template <int TM, int TN, int WM, int WN, bool B128, bool A5, typename CT>
 __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Gemm8Args g, int tiles_m, int tiles_n)
 {
     constexpr bool WIDE = sizeof(CT) == 4;
     constexpr int NW = WM * WN, BM = 16 * TM * WM, BN = 16 * TN * WN;
     constexpr int kStage = (BM + BN) * kBlock8, kLoadsA = BM / (8 * NW), kLoadsB = BN / (8 * NW);
-    constexpr int kScales = B128 ? BM : BM + BN;  // of a stage; a wave fetches 64 of them
-    static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && kScales <= 64 * NW && kScales % 64 == 0, "the loads divide among the waves");
-    __shared__ __attribute__((aligned(1024))) char smem[2 * kStage];
-    __shared__ __attribute__((aligned(16))) float scales[2][kScales];
+    // groups of A that are in registers or on their way there: four, or what the sums and B's scales leave room for
+    constexpr int kAhead = TM == 8 && !B128 ? 2 : 4;
+    constexpr int kScales = B128 ? BM + 64 : BM + BN;  // of a stage (in whole waves' fetches)
+    static_assert(kScales * 4 <= kScaleStage && (2 * kStage) % (2 * kScaleStage) == 0 && (kStage & (kStage - 1)) == 0, "stages differ in one bit");
+    static_assert(kLoadsA == 4 && kLoadsB == 4 && kScales <= 64 * NW, "the loads divide among the waves");
+    static_assert((TM == 4 || TM == 8) && kBlock8 % (16 * TN) == 0, "the schedule of the loads; a wave's rows of B in one tile of scales");
+    // (one array of dynamic size: of several the compiler knows that a load into LDS and a read are of the same one, and waits
+    // for every load in flight before each read, whatever their places in it)
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    char *const scales = smem + 2 * kStage;  // two stages of kScaleStage bytes
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const int64_t bz = blockIdx.y;
     int tm, tn;
     tile_of_block(blockIdx.x, tiles_m, tiles_n, tm, tn);
+    tm = __builtin_amdgcn_readfirstlane(tm), tn = __builtin_amdgcn_readfirstlane(tn);  // (divisions leave vector registers)
     const int m0 = tm * BM, n0 = tn * BN;
     const int rows_m = min(BM, g.M - m0), rows_n = min(BN, g.N - n0);
     const int blocks = (g.K + kBlock8 - 1) / kBlock8;
-    const rsrc_t ra = operand_rsrc(g.A + bz * g.strideA + (int64_t)m0 * g.lda, rows_m, g.lda, g.K);
-    const rsrc_t rb = operand_rsrc(g.B + bz * g.strideB + (int64_t)n0 * g.ldb, rows_n, g.ldb, g.K);
-    // this lane's row and chunk in each of its wave's loads of 8 rows; the offset moves on by a block per step
-    uint32_t off[kLoadsA + kLoadsB];
-#pragma unroll
-    for (int i = 0; i < kLoadsA + kLoadsB; ++i) {
-        const bool is_a = i < kLoadsA;
-        const int row = ((is_a ? i : i - kLoadsA) * NW + wave) * 8 + (lane >> 3);
-        off[i] = (uint32_t)(min(row, (is_a ? rows_m : rows_n) - 1) * (is_a ? g.lda : g.ldb)) + (((lane & 7) ^ swz64(row)) << 4);
+    const uint8_t *tile_a = g.A + bz * g.strideA + (int64_t)m0 * g.lda, *tile_b = g.B + bz * g.strideB + (int64_t)n0 * g.ldb;
+    const int bytes_a = operand_bytes(rows_m, g.lda, g.K), bytes_b = operand_bytes(rows_n, g.ldb, g.K);
+    // this lane's row and chunk in a load of its wave: 8 rows; the wave's loads of a block are 8 NW rows apart
+    const int row = wave * 8 + (lane >> 3), chunk_at = ((lane & 7) ^ swz64(row)) << 4;
+    const uint32_t off_a = (uint32_t)(row * g.lda) + chunk_at, off_b = (uint32_t)(row * g.ldb) + chunk_at;
+    static_assert(NW * 8 % 16 == 0, "the permutation repeats after 16 rows");
+    // the row of scales that this lane fetches for all: A's, then B's, of which a tile of B128 has one for 128 rows
+    const int slot = wave * 64 + lane;
+    const bool fetches = wave * 64 < kScales;
+    const float *my_scale = g.sa + bz * g.strideSA + (int64_t)(m0 + min(slot, rows_m - 1)) * g.ldsa;
+    if (slot >= BM) {
+        const int n = B128 ? min(n0 / kBlock8 + slot - BM, (g.N - 1) / kBlock8) : n0 + min(slot - BM, rows_n - 1);
+        my_scale = g.sb + bz * g.strideSB + (int64_t)n * g.ldsb;
     }
-    const float *my_scale = nullptr;  // the row of scales that this lane fetches for all
-    if (wave * 64 < kScales) {
-        const int s = wave * 64 + lane;
-        if (s < BM)
-            my_scale = g.sa + bz * g.strideSA + (int64_t)(m0 + min(s, rows_m - 1)) * g.ldsa;
-        else
-            my_scale = g.sb + bz * g.strideSB + (int64_t)(n0 + min(s - BM, rows_n - 1)) * g.ldsb;
+    // Load i of a block begins with row 8 NW i and ends with the operand: what is behind (rows past the matrix among it) reads
+    // as zero.  A load of a block past the last one is out of range altogether: it moves nothing, and the number in flight is
+    // the same.
+    rsrc_t from_a[kLoadsA], from_b[kLoadsB];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int skip_a = i * NW * 8 * (int)g.lda, skip_b = i * NW * 8 * (int)g.ldb;
+        from_a[i] = make_rsrc(tile_a + skip_a, max(bytes_a - skip_a, 0));
+        from_b[i] = make_rsrc(tile_b + skip_b, max(bytes_b - skip_b, 0));
     }
-    const float *sb128 = g.sb + bz * g.strideSB + (int64_t)min((n0 + wn * 16 * TN) / kBlock8, (g.N - 1) / kBlock8) * g.ldsb;
-
-    auto issue = [&](int kb) {
-        char *stage = smem + (kb & 1) * kStage;
-#pragma unroll
-        for (int i = 0; i < kLoadsA + kLoadsB; ++i) {
-            const bool is_a = i < kLoadsA;
-            issue_load_to(is_a ? ra : rb, off[i], 0, stage + (is_a ? 0 : BM * kBlock8) + ((is_a ? i : i - kLoadsA) * NW + wave) * 1024);
-            off[i] += kBlock8;
-        }
+    auto load = [&](int kb, int i) {
+        const uint32_t at = kb < blocks ? (uint32_t)kb * kBlock8 : kOutOfRange;
+        char *to = smem + (kb & 1) * kStage + (i * NW + wave) * 1024;
+        issue_load_to(from_a[i], off_a + at, 0, to);
+        issue_load_to(from_b[i], off_b + at, 0, to + BM * kBlock8);
     };
-    float4_t acc[TM][TN];
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = float4_t{0.f, 0.f, 0.f, 0.f};
-
-    auto read = [&](const char *rows, int row, auto mask, int left) {
-        constexpr bool MASK = decltype(mask)::value;
-        int4v_t half[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int chunk = (lane >> 4) + 4 * h;
-            half[h] = *reinterpret_cast<const int4v_t *>(rows + frag_offset64(row + (lane & 15), chunk));
-            if constexpr (MASK) half[h] = keep_first(half[h], left - 16 * chunk);
-        }
-        return int8v_t{half[0][0], half[0][1], half[0][2], half[0][3], half[1][0], half[1][1], half[1][2], half[1][3]};
+    float next_scale;
+    auto load_scale = [&](int kb) { next_scale = my_scale[min(kb, blocks - 1)]; };
+    auto put_scale = [&](int kb) {
+        if (fetches) *reinterpret_cast<float *>(scales + (kb & 1) * kScaleStage + slot * 4) = next_scale;
     };
-    float next_scale = my_scale ? my_scale[0] : 0.f, next128 = B128 ? sb128[0] : 0.f;
+
+    // This lane's places in a stage: of its half fragments of A and B (rows are 16 apart from group to group, which leaves the
+    // permutation as it is) and of the scales of its row of A and its four of B.  They change stages by one bit.
+    const int row_a = wm * 16 * TM, row_b = BM + wn * 16 * TN;
+    int at_a[2], at_b[2], at_sa = 2 * kStage + (row_a + (lane & 15)) * 4;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        at_a[h] = row_a * kBlock8 + frag_offset64(lane & 15, (lane >> 4) + 4 * h);
+        at_b[h] = row_b * kBlock8 + frag_offset64(lane & 15, (lane >> 4) + 4 * h);
+    }
+    const int at_sb = B128 ? (BM + wn * 16 * TN / kBlock8) * 4 : (row_b + 4 * (lane >> 4)) * 4;  // from the stage's scales on
+    auto other_stage = [&](int (&at)[2]) { at[0] ^= kStage, at[1] ^= kStage; };
+    auto read = [&](const int (&at)[2], int row) {
+        const int4v_t lo = *reinterpret_cast<const int4v_t *>(smem + at[0] + row * kBlock8);
+        const int4v_t hi = *reinterpret_cast<const int4v_t *>(smem + at[1] + row * kBlock8);
+        return int8v_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    };
+    auto masked = [&](int8v_t v, int left) {
+        const int4v_t lo = keep_first(int4v_t{v[0], v[1], v[2], v[3]}, left - 16 * (lane >> 4));
+        const int4v_t hi = keep_first(int4v_t{v[4], v[5], v[6], v[7]}, left - 16 * (lane >> 4) - 64);
+        return int8v_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    };
+    int8v_t a[kAhead], b[TN];
+    float fa[kAhead], next128 = 1.f;
+    auto read_a = [&](int i) {
+        a[i % kAhead] = read(at_a, 16 * i);
+        fa[i % kAhead] = *reinterpret_cast<const float *>(smem + at_sa + 64 * i);
+    };
+    auto read_128 = [&](int kb) {
+        if constexpr (B128) next128 = *reinterpret_cast<const float *>(scales + (kb & 1) * kScaleStage + at_sb);
+    };
+
+    static_assert(TN == 4, "the order of the sums");
+    float4_t acc[TM][TN], p[TN], fb[TN];  // p: the last four sums, not yet added
+    float factor = 0.f;                   // of the group before
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) acc[i][j] = float4_t{0.f, 0.f, 0.f, 0.f};
+        p[j] = fb[j] = float4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    auto add = [&](int i, int j, float f) {  // sum j of group i; the empty asm keeps the compiler from doing it earlier or later
+        asm volatile("" : "+v"(p[j]));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (B128)
+                acc[i][j][e] = __builtin_fmaf(p[j][e], f, acc[i][j][e]);
+            else
+                acc[i][j][e] = __builtin_fmaf(p[j][e] * f, fb[j][e], acc[i][j][e]);
+        }
+        asm volatile("" : "+v"(acc[i][j]));
+    };
+
+    // the first two blocks; the first is waited for
+    load_scale(0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) load(0, i);
+    wait_vmem<0>();
+    put_scale(0);
+    wait_vmem_and_lds<0>();
+    wg_barrier();
+    load_scale(1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) load(1, i);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) b[j] = read(at_b, 16 * j);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) read_a(i);
+    read_128(0);
+
+    // a group's first sum: with a step's first one begin its scales of B
+    auto add_first = [&](auto group, int kb, float f) {
+        constexpr int i = decltype(group)::value;
+        if constexpr (i == 0 && !B128) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j) fb[j] = *reinterpret_cast<const float4_t *>(scales + (kb & 1) * kScaleStage + at_sb + 64 * j);
+        }
+        add(i, 0, f);
+    };
     auto step = [&](int kb, auto mask) {
-        if (my_scale) scales[kb & 1][wave * 64 + lane] = next_scale;
-        const float s128 = next128;
-        wait_vmem_and_lds<0>();  // this wave's share of the stage has landed, and its scales
-        wg_barrier();            // everyone's; and everyone has left the other stage
-        if (kb + 1 < blocks) {
-            issue(kb + 1);
-            if (my_scale) next_scale = my_scale[kb + 1];
-            if constexpr (B128) next128 = sb128[kb + 1];
-        }
-        const char *rows_a = smem + (kb & 1) * kStage, *rows_b = rows_a + BM * kBlock8;
-        const float *sa = scales[kb & 1] + wm * 16 * TM;
+        constexpr bool MASK = decltype(mask)::value;
         const int left = g.K - kb * kBlock8;
-        Fragment<WIDE> b[TN];
-        float4_t fb[TN];
-#pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            b[j] = as_fragment<WIDE, false>(read(rows_b, wn * 16 * TN + 16 * j, mask, left));
-            if constexpr (!B128) fb[j] = *reinterpret_cast<const float4_t *>(scales[kb & 1] + BM + wn * 16 * TN + 16 * j + 4 * (lane >> 4));
-        }
-#pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            const Fragment<WIDE> a = as_fragment<WIDE, A5>(read(rows_a, wm * 16 * TM + 16 * i, mask, left));
-            const float fa = sa[16 * i + (lane & 15)];
-#pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                const float4_t p = mma_block<WIDE, A5>(b[j], a);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float f = s128;
-                    if constexpr (!B128) f = fb[j][e];
-                    acc[i][j][e] = __builtin_fmaf(p[e] * fa, f, acc[i][j][e]);
+        int exponent = 127;
+        float mantissa = 1.f;
+        if constexpr (B128) {
+            const uint32_t bits = __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, next128));
+            mantissa = __builtin_bit_cast(float, bits);
+            if constexpr (!WIDE) {
+                if (bits & 0x7f800000u) {  // (zero and subnormal numbers stay whole in the factor)
+                    exponent = (bits >> 23) & 0xff;
+                    mantissa = __builtin_bit_cast(float, (bits & 0x807fffffu) | 0x3f800000u);
                 }
             }
         }
+        Fragment<WIDE> fragment_b[WIDE ? TN : 1];
+        if constexpr (MASK) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j) b[j] = masked(b[j], left);
+        }
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j) fragment_b[j] = as_fragment<WIDE, false>(b[j]);
+        }
+        unrolled<TM>([&](auto group) {
+            constexpr int i = decltype(group)::value;
+            if constexpr (i == TM - kAhead) {
+                wait_vmem<0>();
+                put_scale(kb + 1);
+                wait_lds();
+                wg_barrier();
+                load_scale(kb + 2);
+            }
+            if constexpr (i >= TM - kAhead) {
+#pragma unroll
+                for (int l = 0; l < 4 / kAhead; ++l) load(kb + 2, (i - (TM - kAhead)) * (4 / kAhead) + l);
+            }
+            if constexpr (MASK) a[i % kAhead] = masked(a[i % kAhead], left);
+            const Fragment<WIDE> fragment_a = as_fragment<WIDE, A5>(a[i % kAhead]);
+            const float f = fa[i % kAhead] * mantissa;
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                if constexpr (WIDE) {
+                    p[j] = mma_block<WIDE, A5>(fragment_b[j], fragment_a);
+                } else {
+                    Fragment<false> whole;
+                    whole.v = b[j];
+                    p[j] = mma_block<WIDE, A5>(whole, fragment_a, exponent);
+                }
+                asm volatile("" : "+v"(p[j]));  // (the product is begun here)
+                if constexpr (i == TM - 1) {
+                    if (j == 0) other_stage(at_b);
+                    b[j] = read(at_b, 16 * j);
+                }
+                if (j == TN - 1) {
+                    if constexpr (i == TM - kAhead) other_stage(at_a), at_sa ^= kScaleStage;
+                    read_a((i + kAhead) % TM);
+                    if constexpr (i == TM - 1) read_128(kb + 1);
+                }
+                if (j < TN - 1)
+                    add((i + TM - 1) % TM, j + 1, factor);  // of the group before, or of the step before
+                else
+                    add_first(std::integral_constant<int, i>{}, kb, f);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            factor = f;
+        });
     };
-    issue(0);
     const int whole = g.K / kBlock8;
     for (int kb = 0; kb < whole; ++kb) step(kb, std::false_type{});
     if (whole < blocks) step(whole, std::true_type{});
+#pragma unroll
+    for (int j = 1; j < TN; ++j) add(TM - 1, j, factor);
 
-    CT *C = (CT *)g.C + bz * g.strideC;
+    // C through this wave's part of LDS, so that it leaves 16 bytes per lane in whole rows of 16 TN columns: written from the
+    // registers, 8 or 16 bytes per lane in 16 rows, it took 10 to 17 thousand cycles of the 126 thousand of 4096 x 4096 x 4096.
+    wait_vmem_and_lds<0>();
+    wg_barrier();  // (everyone's loads into LDS have ended)
+    constexpr int kPer = 16 / (int)sizeof(CT), kChunks = 16 * TN / kPer, kRowsOut = 64 / kChunks;
+    static_assert(NW * 16 * TM * 16 * TN * (int)sizeof(CT) <= 2 * kStage, "the tile fits the stages");
+    char *const out = smem + wave * (16 * TM * 16 * TN * (int)sizeof(CT));
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-        const int m = m0 + wm * 16 * TM + 16 * i + (lane & 15);
+        const int row = 16 * i + (lane & 15);
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
-            const int n = n0 + wn * 16 * TN + 16 * j + 4 * (lane >> 4);
+            const int n = 16 * j + 4 * (lane >> 4), chunk = (n / kPer) ^ (row & (kChunks - 1));
             const float v[4] = {g.alpha * acc[i][j][0], g.alpha * acc[i][j][1], g.alpha * acc[i][j][2], g.alpha * acc[i][j][3]};
-            if (m < g.M) store_four<CT>(C + (int64_t)m * g.ldc + n, v, g.N - n);
+            char *at = out + (row * kChunks + chunk) * 16;
+            if constexpr (sizeof(CT) == 4)
+                *reinterpret_cast<float4_t *>(at) = float4_t{v[0], v[1], v[2], v[3]};
+            else
+                *reinterpret_cast<uint2_t *>(at + (n % kPer) * 2) = uint2_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
         }
     }
+    wait_lds();
+    asm volatile("" ::: "memory");
+    CT *C = (CT *)g.C + bz * g.strideC;
+    const int chunk = lane % kChunks, n = n0 + wn * 16 * TN + chunk * kPer;
+#pragma unroll
+    for (int r = 0; r < 16 * TM; r += kRowsOut) {
+        const int row_out = r + lane / kChunks, m = m0 + wm * 16 * TM + row_out;
+        const uint4_t v = *reinterpret_cast<const uint4_t *>(out + (row_out * kChunks + (chunk ^ (row_out & (kChunks - 1)))) * 16);
+        if (m >= g.M || n >= g.N) continue;
+        CT *to = C + (int64_t)m * g.ldc + n;
+        if (n + kPer <= g.N) {
+            if constexpr (sizeof(CT) == 4)
+                *reinterpret_cast<uint4_at4 *>(to) = v;
+            else
+                *reinterpret_cast<uint4_at2 *>(to) = v;
+        } else {
+#pragma unroll
+            for (int e = 0; e < kPer - 1; ++e)
+                if (n + e < g.N) {
+                    if constexpr (sizeof(CT) == 4)
+                        reinterpret_cast<uint32_t *>(to)[e] = v[e];
+                    else
+                        to[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+                }
+        }
+    }
+}
+
+// Raises a kernel's limit of dynamic LDS, an idempotent setting, at its first launch on each device.
+template <auto KERNEL>
+static bool allow_lds(int bytes)
+{
+    static std::atomic<uint64_t> done{0};
+    int device = 0;
+    if (hipGetDevice(&device) != hipSuccess) return false;
+    const uint64_t bit = 1ull << (device & 63);
+    if (device < 64 && (done.load(std::memory_order_relaxed) & bit)) return true;
+    if (hipFuncSetAttribute(reinterpret_cast<const void *>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return false;
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return true;
 }
 
 template <int TM, int TN, int WM, int WN, bool A5, typename CT>
@@ -350,10 +528,15 @@ static perf_status launch_tile(const Gemm8Args &g, hipStream_t stream)
         p.A += b * g.strideA, p.B += b * g.strideB, p.sa += b * g.strideSA, p.sb += b * g.strideSB;
         p.C = (CT *)g.C + b * g.strideC;
         const dim3 grid((unsigned)(tiles_m * tiles_n), (unsigned)std::min(kMaxGridYZ, g.batch - b));
-        if (g.b_block_rows == kBlock8)
-            gemm_fp8_tile_kernel<TM, TN, WM, WN, true, A5, CT><<<grid, 64 * WM * WN, 0, stream>>>(p, (int)tiles_m, (int)tiles_n);
-        else
-            gemm_fp8_tile_kernel<TM, TN, WM, WN, false, A5, CT><<<grid, 64 * WM * WN, 0, stream>>>(p, (int)tiles_m, (int)tiles_n);
+        constexpr int BM = 16 * TM * WM, BN = 16 * TN * WN;
+        const int lds = 2 * (BM + BN) * kBlock8 + 2 * kScaleStage;
+        if (g.b_block_rows == kBlock8) {
+            if (!allow_lds<gemm_fp8_tile_kernel<TM, TN, WM, WN, true, A5, CT>>(lds)) return PERF_ERR_LAUNCH;
+            gemm_fp8_tile_kernel<TM, TN, WM, WN, true, A5, CT><<<grid, 64 * WM * WN, lds, stream>>>(p, (int)tiles_m, (int)tiles_n);
+        } else {
+            if (!allow_lds<gemm_fp8_tile_kernel<TM, TN, WM, WN, false, A5, CT>>(lds)) return PERF_ERR_LAUNCH;
+            gemm_fp8_tile_kernel<TM, TN, WM, WN, false, A5, CT><<<grid, 64 * WM * WN, lds, stream>>>(p, (int)tiles_m, (int)tiles_n);
+        }
         const perf_status st = launch_status();
         if (st != PERF_OK) return st;
     }

@@ -133,14 +133,21 @@ def test_gemm_against_the_definition(m, n, k, b_rows):
     _check_gemm(m, n, k, b_rows, BF16, E5M2, alpha=-0.37)
 
 
-@pytest.mark.parametrize("m,n,k", [(7, 130, 200), (200, 140, 300), (600, 520, 333)])
+@pytest.mark.parametrize("m,n,k", [(1930, 1800, 400), (2049, 1921, 129), (1900, 1920, 128), (3700, 3601, 300), (3585, 3841, 77)])
+@pytest.mark.parametrize("b_rows", [1, 128])
+def test_gemm_of_many_tiles(m, n, k, b_rows):
+    _check_gemm(m, n, k, b_rows, BF16)
+    _check_gemm(m, n, k, b_rows, F32, E5M2)
+
+
+@pytest.mark.parametrize("m,n,k", [(7, 130, 200), (200, 140, 300), (600, 520, 333), (1930, 1800, 333)])
 def test_gemm_with_strides(m, n, k):
     for c_dt in (F32, BF16):
         _check_gemm(m, n, k, 1, c_dt, lda=368, ldb=400, ldsa=5, ldsb=7, ldc=n + 3)
         _check_gemm(m, n, k, 128, c_dt, lda=432, ldb=384, ldsa=4, ldsb=9, ldc=n + 1)
 
 
-@pytest.mark.parametrize("m,n,k,b_rows", [(1, 40, 384, 128), (50, 70, 257, 1), (300, 260, 640, 128), (520, 1040, 515, 1)])
+@pytest.mark.parametrize("m,n,k,b_rows", [(1, 40, 384, 128), (50, 70, 257, 1), (300, 260, 640, 128), (520, 1040, 515, 1), (1800, 1937, 270, 128)])
 def test_gemm_exact_integers(m, n, k, b_rows):
     """Small whole numbers and scales that are powers of two: every sum is exact, in any order, so the result is too."""
     g = np.random.default_rng(m + n + k)
@@ -152,7 +159,7 @@ def test_gemm_exact_integers(m, n, k, b_rows):
     assert np.array_equal(F.run_gemm(a, sa, b, sb, b_rows, F32), ref)
 
 
-@pytest.mark.parametrize("m,n,k", [(3, 40, 130), (150, 130, 261), (520, 1040, 515)])
+@pytest.mark.parametrize("m,n,k", [(3, 40, 130), (150, 130, 261), (520, 1040, 515), (1930, 1801, 261)])
 def test_gemm_does_not_use_what_lies_behind_a_row(m, n, k):
     """Rows' padding full of NaN (0x7f in e4m3) and scales behind the last block of a row: no effect."""
     g = np.random.default_rng(m)
@@ -170,9 +177,14 @@ def test_gemm_does_not_use_what_lies_behind_a_row(m, n, k):
                        1, c_dt=F32, stream=G.stream())
     torch.cuda.synchronize()
     P.assert_contraction_close(c.cpu().numpy(), ref, absdot, k + 3)
+    cb = torch.empty((m, n), dtype=torch.bfloat16, device="cuda")
+    perf.perf_gemm_fp8(ad.data_ptr(), sad.data_ptr(), bd.data_ptr(), sbd.data_ptr(), cb.data_ptr(), m, n, k, ld, kb + 3, ld, kb + 3, n,
+                       1, c_dt=BF16, stream=G.stream())
+    torch.cuda.synchronize()
+    P.assert_contraction_close(cb.cpu().double().numpy(), ref, absdot, k + 3 + 2 ** 13, out_bf16=True)
 
 
-@pytest.mark.parametrize("m,n,k,batch", [(1, 200, 256, 3), (40, 72, 130, 5), (256, 256, 384, 9), (300, 520, 200, 2)])
+@pytest.mark.parametrize("m,n,k,batch", [(1, 200, 256, 3), (40, 72, 130, 5), (256, 256, 384, 9), (300, 520, 200, 2), (515, 700, 300, 11)])
 def test_gemm_batch(m, n, k, batch):
     g = np.random.default_rng(batch)
     ops = [(F.random_operand(g, m, k, 1), F.random_operand(g, n, k, 128)) for _ in range(batch)]
@@ -215,7 +227,7 @@ def test_gemm_shared_operand_in_a_batch():
         P.assert_contraction_close(c[i].cpu().numpy(), ref, absdot, k + 3)
 
 
-@pytest.mark.parametrize("m,n,k", [(1, 64, 256), (200, 300, 256), (600, 1100, 256)])
+@pytest.mark.parametrize("m,n,k", [(1, 64, 256), (200, 300, 256), (1900, 1920, 256)])
 def test_gemm_scales_whose_product_leaves_fp32(m, n, k):
     """Scales of 2^-80 and of 2^90: their products alone are no normal numbers, the results are."""
     g = np.random.default_rng(1)
