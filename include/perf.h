@@ -253,7 +253,7 @@ perf_status perf_quantize_fp8(const void *x, void *q, float *scales, void *qt, f
  * The last block may be short; what lies in memory behind a row's K elements is not used.
  * Errors: NULL, SHAPE (dimension < 1 or > 2^30, ld too small, negative stride, batches overlapping in C, b_block_rows not 1
  * or 128), DTYPE, ALIGN (A or B not 16-byte aligned, scales or C not aligned to their elements), UNSUPPORTED (b_dt E5M2; lda,
- * ldb, strideA or strideB not a multiple of 16, or lda or ldb of 2^23 or more), LAUNCH. */
+ * ldb, strideA or strideB not a multiple of 16, or a row stride of A, B or their scales of 2^23 or more), LAUNCH. */
 perf_status perf_gemm_fp8(const void *A, const float *scaleA, const void *B, const float *scaleB, void *C, int64_t M, int64_t N,
                           int64_t K, int64_t lda, int64_t ldsa, int64_t ldb, int64_t ldsb, int64_t ldc, int64_t b_block_rows,
                           int64_t batch, int64_t strideA, int64_t strideSA, int64_t strideB, int64_t strideSB, int64_t strideC,

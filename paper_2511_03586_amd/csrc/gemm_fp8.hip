@@ -88,32 +88,11 @@ __device__ __forceinline__ int4v_t keep_first(int4v_t v, int n)
     return v;
 }
 
-// An operand's rows as a buffer that ends with the last row's last element, rounded up to whole words (a word that holds an
-// element is readable): what lies behind reads as zero.  Rows of a tile past the matrix read its last row instead.
-__device__ __forceinline__ uint32_t operand_bytes(int rows, int64_t ld, int K)
+// Bytes of an operand's rows as a buffer: to the last row's last element, rounded up to whole words (a word that holds an
+// element is readable).  What lies behind reads as zero.
+__device__ __forceinline__ int operand_bytes(int rows, int64_t ld, int K)
 {
-    return (uint32_t)(((int64_t)(rows - 1) * ld + K + 3) & ~(int64_t)3);
-}
-__device__ __forceinline__ rsrc_t operand_rsrc(const uint8_t *base, int rows, int64_t ld, int K)
-{
-    return make_rsrc(base, operand_bytes(rows, ld, K));
-}
-
-// A lane's 32 elements of a row in a block: the 16 from 16 * (lane / 16) on, and those 64 further on.  `left`: elements of
-// the row from the block's start on; with MASK those behind it are cleared (a row's padding may hold anything).
-template <bool MASK>
-__device__ __forceinline__ int8v_t load_fragment(rsrc_t rsrc, uint32_t row_offset, uint32_t block_offset, int lane, int left)
-{
-    const int k = 16 * (lane >> 4);
-    int4v_t half[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        // (the range check is sure to see the whole offset where it matters: in a short block it is all the lane's)
-        half[h] = __builtin_bit_cast(int4v_t, __builtin_amdgcn_raw_buffer_load_b128(rsrc, row_offset + k + 64 * h + (MASK ? block_offset : 0),
-                                                                                  MASK ? 0 : block_offset, 0));
-        if constexpr (MASK) half[h] = keep_first(half[h], left - (k + 64 * h));
-    }
-    return int8v_t{half[0][0], half[0][1], half[0][2], half[0][3], half[1][0], half[1][1], half[1][2], half[1][3]};
+    return (int)(((int64_t)(rows - 1) * ld + K + 3) & ~(int64_t)3);
 }
 
 template <typename CT> __device__ __forceinline__ void store_four(CT *p, const float (&v)[4], int n);
@@ -138,75 +117,124 @@ template <> __device__ __forceinline__ void store_four<uint16_t>(uint16_t *p, co
     }
 }
 
-// TM x TN groups of 16 rows of A and of B per workgroup; W waves, wave w takes the blocks w, w + W, ...
-template <int TM, int TN, int W, bool A5, typename CT>
-__global__ __launch_bounds__(64 * W) void gemm_fp8_waves_kernel(const Gemm8Args g, int tiles_m)
+// A half fragment's elements behind the row's end are cleared: `left` of them from the block's start on are inside.
+__device__ __forceinline__ int8v_t masked_fragment(int8v_t v, int left, int lane)
 {
-    __shared__ float4_t sums[W][TM * TN][64];
+    const int4v_t lo = keep_first(int4v_t{v[0], v[1], v[2], v[3]}, left - 16 * (lane >> 4));
+    const int4v_t hi = keep_first(int4v_t{v[4], v[5], v[6], v[7]}, left - 16 * (lane >> 4) - 64);
+    return int8v_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+}
+
+// All of this wave's LDS accesses are done; its loads stay in flight.
+__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xC07F); }
+
+// TM x TN groups of 16 rows of A and of B per workgroup; its W waves take every W-th block of K, each through NS stages of LDS
+// of its own, and meet no barrier until their sums are added.  A stage: the rows, 128 bytes each, loaded eight lanes to a row
+// (a load of 16 bytes from each of 16 rows, as the fragments lie, moves a third of that per clock) with their chunks permuted
+// (swz64), then the scales, loaded a lane to a row.
+constexpr int waves_stage_bytes(int TM, int TN) { return (TM + TN) * 16 * kBlock8 + 512; }
+
+template <int TM, int TN, int W, int NS, bool B128, bool A5, typename CT>
+__global__ __launch_bounds__(64 * W) void gemm_fp8_waves_kernel(const Gemm8Args g, int tiles_m, int tiles_n)
+{
     constexpr bool WIDE = sizeof(CT) == 4;
+    constexpr int kStage = waves_stage_bytes(TM, TN), kLoads = 2 * (TM + TN) + 2;  // loads of a stage
+    extern __shared__ __attribute__((aligned(1024))) char smem[];  // (one array, as in the tile kernel)
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t bz = blockIdx.y;
-    // (divisions leave vector registers)
-    const int tile_n = __builtin_amdgcn_readfirstlane((int)blockIdx.x / tiles_m), tile_m = (int)blockIdx.x - tile_n * tiles_m;
-    const int m0 = tile_m * 16 * TM, n0 = tile_n * 16 * TN;
+    int tm, tn;
+    tile_of_block(blockIdx.x, tiles_m, tiles_n, tm, tn);
+    tm = __builtin_amdgcn_readfirstlane(tm), tn = __builtin_amdgcn_readfirstlane(tn);  // (divisions leave vector registers)
+    const int m0 = tm * 16 * TM, n0 = tn * 16 * TN;
     const int rows_m = min(16 * TM, g.M - m0), rows_n = min(16 * TN, g.N - n0);
     const int blocks = (g.K + kBlock8 - 1) / kBlock8;
-    const rsrc_t ra = operand_rsrc(g.A + bz * g.strideA + (int64_t)m0 * g.lda, rows_m, g.lda, g.K);
-    const rsrc_t rb = operand_rsrc(g.B + bz * g.strideB + (int64_t)n0 * g.ldb, rows_n, g.ldb, g.K);
-    const float *sa = g.sa + bz * g.strideSA, *sb = g.sb + bz * g.strideSB;
-    uint32_t a_off[TM], b_off[TN];
-    const float *sa_row[TM], *sb_row[TN][4];
+    const uint8_t *tile_a = g.A + bz * g.strideA + (int64_t)m0 * g.lda, *tile_b = g.B + bz * g.strideB + (int64_t)n0 * g.ldb;
+    const int bytes_a = operand_bytes(rows_m, g.lda, g.K), bytes_b = operand_bytes(rows_n, g.ldb, g.K);
+    rsrc_t from_a[2 * TM], from_b[2 * TN];  // the operand from row 8 i on
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int r = min(16 * i + (lane & 15), rows_m - 1);
-        a_off[i] = (uint32_t)(r * g.lda);
-        sa_row[i] = sa + (int64_t)(m0 + r) * g.ldsa;
-    }
+    for (int i = 0; i < 2 * TM; ++i) from_a[i] = make_rsrc(tile_a + (int64_t)(8 * i) * g.lda, max(bytes_a - 8 * i * (int)g.lda, 0));
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-        b_off[j] = (uint32_t)(min(16 * j + (lane & 15), rows_n - 1) * g.ldb);
+    for (int i = 0; i < 2 * TN; ++i) from_b[i] = make_rsrc(tile_b + (int64_t)(8 * i) * g.ldb, max(bytes_b - 8 * i * (int)g.ldb, 0));
+    // rows 8 i + lane / 8: the permutation of odd i is that of even i with its third bit turned
+    const uint32_t chunk = (lane & 7) ^ swz64(lane >> 3), row8 = lane >> 3;
+    const uint32_t off_a[2] = {(uint32_t)(row8 * g.lda) + chunk * 16, (uint32_t)(row8 * g.lda) + (chunk ^ 4) * 16};
+    const uint32_t off_b[2] = {(uint32_t)(row8 * g.ldb) + chunk * 16, (uint32_t)(row8 * g.ldb) + (chunk ^ 4) * 16};
+    const rsrc_t scales_a = make_rsrc(g.sa + bz * g.strideSA + (int64_t)m0 * g.ldsa, (uint32_t)(((rows_m - 1) * g.ldsa + blocks) * 4));
+    const int first_b = B128 ? n0 / kBlock8 : n0, last_b = B128 ? (n0 + rows_n - 1) / kBlock8 : n0 + rows_n - 1;
+    const rsrc_t scales_b = make_rsrc(g.sb + bz * g.strideSB + (int64_t)first_b * g.ldsb, (uint32_t)(((last_b - first_b) * g.ldsb + blocks) * 4));
+    const uint32_t off_sa = (uint32_t)(min(lane, rows_m - 1) * g.ldsa * 4);
+    const uint32_t off_sb = (uint32_t)(((B128 ? (n0 + min(lane, rows_n - 1)) / kBlock8 : n0 + min(lane, rows_n - 1)) - first_b) * g.ldsb * 4);
+
+    char *const mine = smem + wave * NS * kStage;
+    auto load = [&](int kb, int stage) {  // past the last block out of range: nothing is moved, the number in flight is the same
+        const uint32_t at = kb < blocks ? (uint32_t)kb * kBlock8 : kOutOfRange, at_s = kb < blocks ? (uint32_t)kb * 4 : kOutOfRange;
+        char *to = mine + stage * kStage;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int n = n0 + min(16 * j + 4 * (lane >> 4) + e, rows_n - 1);
-            sb_row[j][e] = sb + (int64_t)(n / g.b_block_rows) * g.ldsb;
-        }
-    }
+        for (int i = 0; i < 2 * TM; ++i) issue_load_to(from_a[i], off_a[i & 1] + at, 0, to + i * 1024);
+#pragma unroll
+        for (int i = 0; i < 2 * TN; ++i) issue_load_to(from_b[i], off_b[i & 1] + at, 0, to + (2 * TM + i) * 1024);
+        to += (TM + TN) * 16 * kBlock8;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(scales_a, (__attribute__((address_space(3))) void *)to, 4, off_sa + at_s, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(scales_b, (__attribute__((address_space(3))) void *)(to + 256), 4, off_sb + at_s, 0, 0, 0);
+    };
     float4_t acc[TM][TN];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = float4_t{0.f, 0.f, 0.f, 0.f};
-    auto block = [&](int kb, auto mask) {
-        constexpr bool MASK = decltype(mask)::value;
+    const int place[2] = {frag_offset64(lane & 15, lane >> 4), frag_offset64(lane & 15, (lane >> 4) + 4)};
+    auto block = [&](int kb, int stage) {
+        wait_vmem<(NS - 1) * kLoads>();  // the stage has arrived
+        asm volatile("" ::: "memory");
+        const char *at = mine + stage * kStage;
+        auto read = [&](int group) {
+            const int4v_t lo = *reinterpret_cast<const int4v_t *>(at + group * 16 * kBlock8 + place[0]);
+            const int4v_t hi = *reinterpret_cast<const int4v_t *>(at + group * 16 * kBlock8 + place[1]);
+            return int8v_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        };
+        int8v_t raw_a[TM], raw_b[TN];
+        float fa[TM];
+        float4_t fb[TN];
+        const char *scales = at + (TM + TN) * 16 * kBlock8;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) raw_a[i] = read(i), fa[i] = *reinterpret_cast<const float *>(scales + (16 * i + (lane & 15)) * 4);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) raw_b[j] = read(TM + j), fb[j] = *reinterpret_cast<const float4_t *>(scales + 256 + (16 * j + 4 * (lane >> 4)) * 4);
+        wait_lds();  // it is in registers: the stage is free
+        asm volatile("" ::: "memory");
+        load(kb + NS * W, stage);
         const int left = g.K - kb * kBlock8;
-        int8v_t ra_[TM], rb_[TN];
-        float fa[TM], fb[TN][4];
+        if (left < kBlock8) {
 #pragma unroll
-        for (int i = 0; i < TM; ++i) ra_[i] = load_fragment<MASK>(ra, a_off[i], (uint32_t)kb * kBlock8, lane, left), fa[i] = sa_row[i][kb];
+            for (int i = 0; i < TM; ++i) raw_a[i] = masked_fragment(raw_a[i], left, lane);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            rb_[j] = load_fragment<MASK>(rb, b_off[j], (uint32_t)kb * kBlock8, lane, left);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) fb[j][e] = sb_row[j][e][kb];
+            for (int j = 0; j < TN; ++j) raw_b[j] = masked_fragment(raw_b[j], left, lane);
         }
-        Fragment<WIDE> a[TM], b[TN];
+        Fragment<WIDE> b[TN];
 #pragma unroll
-        for (int i = 0; i < TM; ++i) a[i] = as_fragment<WIDE, A5>(ra_[i]);
+        for (int j = 0; j < TN; ++j) b[j] = as_fragment<WIDE, false>(raw_b[j]);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) b[j] = as_fragment<WIDE, false>(rb_[j]);
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
+        for (int i = 0; i < TM; ++i) {
+            const Fragment<WIDE> a = as_fragment<WIDE, A5>(raw_a[i]);
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
-                const float4_t p = mma_block<WIDE, A5>(b[j], a[i]);
+                const float4_t p = mma_block<WIDE, A5>(b[j], a);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_fmaf(p[e] * fa[i], fb[j][e], acc[i][j][e]);
             }
+        }
     };
-    const int whole = g.K / kBlock8;
-    int kb = wave;
-    for (; kb < whole; kb += W) block(kb, std::false_type{});
-    if (kb < blocks) block(kb, std::true_type{});
+#pragma unroll
+    for (int t = 0; t < NS; ++t) load(wave + t * W, t);
+    for (int kb = wave; kb < blocks; kb += NS * W) {
+#pragma unroll
+        for (int t = 0; t < NS; ++t)
+            if (t == 0 || kb + t * W < blocks) block(kb + t * W, t);
+    }
+    wait_vmem_and_lds<0>();  // (loads into LDS end before its next use)
+    wg_barrier();
+    float4_t(&sums)[W][TM * TN][64] = *reinterpret_cast<float4_t(*)[W][TM * TN][64]>(smem);
+    static_assert(sizeof(sums) <= W * NS * kStage, "the sums fit the stages");
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -225,9 +253,6 @@ __global__ __launch_bounds__(64 * W) void gemm_fp8_waves_kernel(const Gemm8Args 
 }
 
 constexpr int kScaleStage = 2048;  // bytes of LDS for the scales of a block: one for each row of a tile of A and of B, or for 128 of B
-
-// All of this wave's LDS accesses are done; its loads stay in flight.
-__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xC07F); }
 
 // WM x WN waves, each with TM x TN groups of 16 rows of A and of B.  LDS: two stages of a block of K, rows of 128 bytes whose
 // 16-byte chunks are permuted as in mfma_tile.h (swz64), and the block's scales.
@@ -319,11 +344,6 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Ge
         const int4v_t hi = *reinterpret_cast<const int4v_t *>(smem + at[1] + row * kBlock8);
         return int8v_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     };
-    auto masked = [&](int8v_t v, int left) {
-        const int4v_t lo = keep_first(int4v_t{v[0], v[1], v[2], v[3]}, left - 16 * (lane >> 4));
-        const int4v_t hi = keep_first(int4v_t{v[4], v[5], v[6], v[7]}, left - 16 * (lane >> 4) - 64);
-        return int8v_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-    };
     int8v_t a[kAhead], b[TN];
     float fa[kAhead], next128 = 1.f;
     auto read_a = [&](int i) {
@@ -399,7 +419,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Ge
         Fragment<WIDE> fragment_b[WIDE ? TN : 1];
         if constexpr (MASK) {
 #pragma unroll
-            for (int j = 0; j < TN; ++j) b[j] = masked(b[j], left);
+            for (int j = 0; j < TN; ++j) b[j] = masked_fragment(b[j], left, lane);
         }
         if constexpr (WIDE) {
 #pragma unroll
@@ -418,7 +438,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Ge
 #pragma unroll
                 for (int l = 0; l < 4 / kAhead; ++l) load(kb + 2, (i - (TM - kAhead)) * (4 / kAhead) + l);
             }
-            if constexpr (MASK) a[i % kAhead] = masked(a[i % kAhead], left);
+            if constexpr (MASK) a[i % kAhead] = masked_fragment(a[i % kAhead], left, lane);
             const Fragment<WIDE> fragment_a = as_fragment<WIDE, A5>(a[i % kAhead]);
             const float f = fa[i % kAhead] * mantissa;
 #pragma unroll
@@ -543,21 +563,38 @@ static perf_status launch_tile(const Gemm8Args &g, hipStream_t stream)
     return PERF_OK;
 }
 
-template <int TM, int TN, int W, bool A5, typename CT>
+template <int TM, int TN, bool A5, typename CT>
 static perf_status launch_waves(const Gemm8Args &g, hipStream_t stream)
 {
+    constexpr int W = 8, NS = W * 2 * waves_stage_bytes(TM, TN) <= 150 * 1024 ? 2 : 1;
     const int64_t tiles_m = (g.M + 16 * TM - 1) / (16 * TM), tiles_n = (g.N + 16 * TN - 1) / (16 * TN);
     if (tiles_m * tiles_n > max_blocks(64 * W)) return PERF_ERR_UNSUPPORTED;
+    const int lds = W * NS * waves_stage_bytes(TM, TN);
     for (int64_t b = 0; b < g.batch; b += kMaxGridYZ) {
         Gemm8Args p = g;
         p.A += b * g.strideA, p.B += b * g.strideB, p.sa += b * g.strideSA, p.sb += b * g.strideSB;
         p.C = (CT *)g.C + b * g.strideC;
         const dim3 grid((unsigned)(tiles_m * tiles_n), (unsigned)std::min(kMaxGridYZ, g.batch - b));
-        gemm_fp8_waves_kernel<TM, TN, W, A5, CT><<<grid, 64 * W, 0, stream>>>(p, (int)tiles_m);
+        if (g.b_block_rows == kBlock8) {
+            if (!allow_lds<gemm_fp8_waves_kernel<TM, TN, W, NS, true, A5, CT>>(lds)) return PERF_ERR_LAUNCH;
+            gemm_fp8_waves_kernel<TM, TN, W, NS, true, A5, CT><<<grid, 64 * W, lds, stream>>>(p, (int)tiles_m, (int)tiles_n);
+        } else {
+            if (!allow_lds<gemm_fp8_waves_kernel<TM, TN, W, NS, false, A5, CT>>(lds)) return PERF_ERR_LAUNCH;
+            gemm_fp8_waves_kernel<TM, TN, W, NS, false, A5, CT><<<grid, 64 * W, lds, stream>>>(p, (int)tiles_m, (int)tiles_n);
+        }
         const perf_status st = launch_status();
         if (st != PERF_OK) return st;
     }
     return PERF_OK;
+}
+
+template <int TM, bool A5, typename CT>
+static perf_status waves_by_columns(const Gemm8Args &g, hipStream_t stream)
+{
+    const int64_t tiles_m = (g.M + 16 * TM - 1) / (16 * TM) * g.batch;
+    if (tiles_m * ((g.N + 63) / 64) >= 200) return launch_waves<TM, 4, A5, CT>(g, stream);
+    if (tiles_m * ((g.N + 31) / 32) >= 200) return launch_waves<TM, 2, A5, CT>(g, stream);
+    return launch_waves<TM, 1, A5, CT>(g, stream);
 }
 
 template <bool A5, typename CT>
@@ -568,8 +605,9 @@ static perf_status gemm8(const Gemm8Args &g, hipStream_t stream)
         if (big >= 200) return launch_tile<8, 4, 2, 4, A5, CT>(g, stream);
     }
     if (mid >= 200) return launch_tile<4, 4, 2, 2, A5, CT>(g, stream);
-    if (g.M <= 16) return launch_waves<1, 1, 8, A5, CT>(g, stream);
-    return launch_waves<2, 2, 8, A5, CT>(g, stream);
+    if (g.M <= 16) return waves_by_columns<1, A5, CT>(g, stream);
+    if (g.M <= 32) return waves_by_columns<2, A5, CT>(g, stream);
+    return waves_by_columns<4, A5, CT>(g, stream);
 }
 
 }  // namespace perf
@@ -591,7 +629,8 @@ extern "C" perf_status perf_gemm_fp8(const void *A, const float *scaleA, const v
     if (!dtype8_ok(a_dt) || !dtype8_ok(b_dt) || !dtype_ok(c_dt)) return PERF_ERR_DTYPE;
     if (!aligned(A, 16) || !aligned(B, 16) || !aligned(scaleA, 4) || !aligned(scaleB, 4) || !aligned(C, dtype_size(c_dt)))
         return PERF_ERR_ALIGN;
-    if (b_dt != PERF_E4M3 || lda % 16 || ldb % 16 || lda >= (1 << 23) || ldb >= (1 << 23)) return PERF_ERR_UNSUPPORTED;
+    if (b_dt != PERF_E4M3 || lda % 16 || ldb % 16 || lda >= (1 << 23) || ldb >= (1 << 23) || ldsa >= (1 << 23) || ldsb >= (1 << 23))
+        return PERF_ERR_UNSUPPORTED;
     if (batch > 1 && (strideA % 16 || strideB % 16)) return PERF_ERR_UNSUPPORTED;
     const Gemm8Args g{(const uint8_t *)A, (const uint8_t *)B, scaleA, scaleB, C, (int)M, (int)N, (int)K, lda, ldsa, ldb, ldsb, ldc,
                       strideA, strideSA, strideB, strideSB, strideC, batch, (int)b_block_rows, alpha};
