@@ -42,7 +42,7 @@ template <bool E5M2> struct Fp8 {
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp_max_u32(uint32_t v)
 {
-    const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xF, 0xF, false);
+    const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);  // (all lanes have a source)
     return v > o ? v : o;
 }
 template <int LANES>
@@ -99,7 +99,15 @@ template <> struct Eight<uint16_t> {
             if (e < n) w[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
         raw = uint4_t{w[0], w[1], w[2], w[3]};
     }
+    // columns in runs, one here, two `far` apart in fp32 (read once); or columns c on, those behind `last` as that one
+    __device__ __forceinline__ void load_runs(const uint16_t *p, int) { load(p, 8); }
+    __device__ __forceinline__ void load_runs(const uint16_t *row, int c, int, int last)
+    {
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) raw[e >> 1] = (uint32_t)row[min(c + e + 1, last)] << 16 | row[min(c + e, last)];
+    }
     __device__ __forceinline__ void get(float (&v)[8]) const { Elem<uint16_t>::unpack(raw, v); }
+    __device__ __forceinline__ float one(int e) const { return e & 1 ? bf16_hi(raw[e >> 1]) : bf16_lo(raw[e >> 1]); }
     __device__ __forceinline__ void get_half(int q, float (&v)[4]) const  // elements 4q .. 4q + 3
     {
         const uint32_t a = raw[2 * q], b = raw[2 * q + 1];
@@ -145,6 +153,18 @@ template <> struct Eight<float> {
         lo = uint4_t{w[0], w[1], w[2], w[3]};
         hi = uint4_t{w[4], w[5], w[6], w[7]};
     }
+    __device__ __forceinline__ void load_runs(const float *p, int far)
+    {
+        lo = __builtin_nontemporal_load(reinterpret_cast<const uint4_at4 *>(p));
+        hi = __builtin_nontemporal_load(reinterpret_cast<const uint4_at4 *>(p + far));
+    }
+    __device__ __forceinline__ void load_runs(const float *row, int c, int far, int last)
+    {
+        const uint32_t *w = reinterpret_cast<const uint32_t *>(row);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) lo[e] = w[min(c + e, last)], hi[e] = w[min(c + far + e, last)];
+    }
+    __device__ __forceinline__ float one(int e) const { return __builtin_bit_cast(float, (uint32_t)(e < 4 ? lo[e & 3] : hi[e & 3])); }
     __device__ __forceinline__ void get_half(int q, float (&v)[4]) const { Elem<float>::unpack(q ? hi : lo, v); }
     __device__ __forceinline__ void get(float (&v)[8]) const
     {

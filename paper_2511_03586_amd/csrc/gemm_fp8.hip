@@ -634,8 +634,10 @@ static perf_status gemm8(const Gemm8Args &g, hipStream_t stream)
     constexpr bool WIDE = sizeof(CT) == 4;
     const int64_t big = ((g.M + 255) / 256) * ((g.N + 255) / 256) * g.batch, mid = ((g.M + 127) / 128) * ((g.N + 127) / 128) * g.batch;
     const int64_t blocks = (g.K + kBlock8 - 1) / kBlock8;
+    // A round of 256 tiles of 256 x 256 takes as long as 2.4 of 128 x 128 (K = 4096, N = 4096: 50 us; 41 for two of the latter, 63
+    // for three), so the larger ones pay from three rounds of the smaller on.
     if constexpr (!WIDE) {
-        if (big >= 200) return launch_tile<8, 4, 2, 4, A5, CT>(g, stream);
+        if (12 * ((big + 255) / 256) < 5 * ((mid + 255) / 256)) return launch_tile<8, 4, 2, 4, A5, CT>(g, stream);
     }
     // A tile kernel on less than the whole chip begins sooner, the waves that divide K then go on faster.  128 tiles: K = 1024
     // 8.8 us against 12.7, K = 4096 26.7 against 23.3 (bf16 C); K = 700 13.0 against 14.1, K = 4096 42 against 29.5 (fp32 C).
