@@ -299,7 +299,7 @@ def run(s):
                            ld, kb, ld, kb, n, case["b_rows"], case["batch"], m * ld, m * kb, n * ld, -(-n // case["b_rows"]) * kb,
                            m * n, 1.0, _CODE[case["a"]], perf.PERF_E4M3, _CODE[case["out"]], stream=st)
         return {"c": s["c"]}
-    rows, cols, dt, gate_rows = case["rows"], case["cols"], _CODE[case["dtype"]], case["gate_rows"] or rows
+    rows, cols, dt, gate_rows = case["rows"], case["cols"], _CODE[case["dtype"]], case["gate_rows"] or case["rows"]
     gate_dt = _CODE[case["gate_dtype"]]
     if op == "norm":
         same = case["out"] == "same"
