@@ -217,6 +217,7 @@ __device__ __forceinline__ void store_bytes(uint8_t *p, const uint32_t (&w)[N / 
 template <typename T, bool RAG> struct Group {
     static constexpr int kRuns = sizeof(T) / 2, kRun = 8 / kRuns;
     int at[kRuns], dup[kRuns];
+    Group() = default;
     __device__ __forceinline__ Group(int lane, int threads, int cols)
     {
 #pragma unroll
@@ -267,17 +268,22 @@ template <typename T, bool RAG> struct Group {
             P *p = offset_by(row, at[r]);
             const float *f = v + kRun * r;
             if (dup[r] == 0) {
-                if constexpr (kRun == 8) {
-                    store_row_chunk<true, P, 8>(p, f);
-                } else {
-                    store_row_chunk<true, P, 4>(p, f);
-                }
+                store_row_chunk<true, P, kRun>(p, f);
             } else if constexpr (RAG) {
 #pragma unroll
                 for (int e = 1; e < kRun; ++e)
                     if (e >= dup[r]) Elem<P>::store1(p + e, f[e]);
             }
         }
+    }
+    // fp32 that this lane reads again
+    __device__ __forceinline__ void store_cached(float *row, const float (&v)[8]) const
+    {
+#pragma unroll
+        for (int r = 0; r < kRuns; ++r)
+#pragma unroll
+            for (int e = 0; e < kRun; ++e)
+                if (dup[r] <= (RAG ? e : 0)) offset_by(row, at[r])[e] = v[kRun * r + e];
     }
     // the eight as bytes w
     __device__ __forceinline__ void store_bytes(uint8_t *row, const uint32_t (&w)[2]) const

@@ -7,13 +7,16 @@
 //     D = gate H,  v = D gamma_post,     du = r1 (v - un mean(v un)),  dgamma_post = sum of D un,  dgate = sum of n H.
 // (gamma_post left out: n = u, du = D.)  Bound by HBM: each operand is read once and each result written once.
 //
-//  * residual_norm_kernel / residual_norm_grad_kernel<W>: W waves own a row, 8 elements per lane, so that a row is in
-//    registers between its two sums; workgroups of 8 waves (gradient: 16) take the rows of several teams side by side.  The gains and the gate are read
-//    once for all rows that share them.
+//  * residual_norm_kernel / residual_norm_grad_kernel<W>: W waves own a row, 8 elements per lane (16 from 8193 columns on), so
+//    that a row is in registers between its two sums; workgroups of 8 waves (gradient: 16) take the rows of several teams
+//    side by side.  The gains and the gate are read once for all rows that share them.
 //  * The gradient's sums over rows: a workgroup owns a run of rows and sums them in registers; its sums go to the
 //    workspace and are added in the order of the rows by residual_norm_sums_kernel.  No atomics.
-//  * residual_norm_any_kernel and its gradient: rows beyond 16 waves' registers, several passes over memory.
+//  * residual_norm_any_kernel and its gradient: rows of fewer than 8 elements and those beyond 16 waves' registers, in several
+//    passes over memory.
 // Statistics, h on its way into y, and all sums are fp32; y is computed from h before it is rounded to its type.
+// Measured (bf16, one gate for all rows): 8192 x 4096 forward 46 us (5.8 TB/s), gradient 80 us (5.0 TB/s, 75 + 5 in its two
+// kernels); 2048 x 16384 50 and 102 us, where several passes over memory took 73 and 530.
 #include "fp8.h"
 #include "host_utils.h"
 
@@ -95,8 +98,8 @@ __device__ __forceinline__ float team_sum(float v, float *red)
     return v;
 }
 
-// Y8: y is e4m3 with scales (else of x's type); RAG: rows that are no whole groups of 8
-template <typename T, int W, bool Y8, bool RAG>
+// G: groups of eight elements per lane.  Y8: y is e4m3 with scales (else of x's type); RAG: rows that are no whole groups of 8
+template <typename T, int W, int G, bool Y8, bool RAG>
 __global__ __launch_bounds__(W > 8 ? 64 * W : 512) void residual_norm_kernel(const NormArgs a)
 {
     constexpr int kWaves = W > 8 ? W : 8, kTeams = kWaves / W, kThreads = 64 * W;
@@ -104,55 +107,76 @@ __global__ __launch_bounds__(W > 8 ? 64 * W : 512) void residual_norm_kernel(con
     // (the same in all lanes of a wave: rows and their addresses are scalars)
     const int team = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / W, lane = threadIdx.x - team * kThreads;
     const float inv_cols = 1.0f / (float)a.cols;
-    const Group<T, RAG> own(lane, kThreads, a.cols);
-    float post[8], pre[8], gate[8];
+    using Own = Group<T, RAG>;
+    Own own[G];
+    float post[G][8], pre[G][8], gate[G][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) post[e] = pre[e] = gate[e] = 1.f;
-    if (a.post.p) a.post.group(0, own, post);
-    if (a.pre.p) a.pre.group(0, own, pre);
+    for (int k = 0; k < G; ++k) {
+        own[k] = Own(lane + k * Own::kRuns * kThreads, kThreads, a.cols);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) post[k][e] = pre[k][e] = gate[k][e] = 1.f;
+        if (a.post.p) a.post.group(0, own[k], post[k]);
+        if (a.pre.p) a.pre.group(0, own[k], pre[k]);
+    }
     int held = -1;  // the group of rows whose gate is in `gate`
     const int step = gridDim.x * kTeams;
-    Eight<T> u, x;
+    constexpr bool kAhead = G * sizeof(T) <= 4;  // (two groups of fp32 leave no registers for the next row's operands)
+    Eight<T> u[G], x[G];
     auto load = [&](int to) {
         const int64_t r = min(to, a.rows - 1);
-        own.load(u, (const T *)a.u + r * a.ldu);
-        own.load(x, (const T *)a.x + r * a.ldx);
+#pragma unroll
+        for (int k = 0; k < G; ++k) {
+            own[k].load(u[k], (const T *)a.u + r * a.ldu);
+            own[k].load(x[k], (const T *)a.x + r * a.ldx);
+        }
     };
     // teams of a workgroup take neighbouring rows and run the same number of rounds: its barriers are met by all
     int at = blockIdx.x * kTeams + team;
-    load(at);
+    if constexpr (kAhead) load(at);
     for (int first = blockIdx.x * kTeams; first < a.rows; first += step, at += step) {
         const int64_t row = at;
         const bool live = at < a.rows;
         if (a.gate.p && live) {
             const int g = div_by(at, a.gate_rows, a.gate_magic);
             if (g != held) {
-                a.gate.group((int64_t)g * a.ldg, own, gate);
+#pragma unroll
+                for (int k = 0; k < G; ++k) a.gate.group((int64_t)g * a.ldg, own[k], gate[k]);
                 held = g;
             }
         }
-        float v[8], h[8], s = 0.f;
-        own.keep(u, true), own.keep(x, true);
-        u.get(v), x.get(h);
-        load(at + step);  // the next row's loads fly during this row's sums
+        if constexpr (!kAhead) load(at);
+        float v[G][8], h[G][8], s = 0.f;
+#pragma unroll
+        for (int k = 0; k < G; ++k) {
+            own[k].keep(u[k], true), own[k].keep(x[k], true);
+            u[k].get(v[k]), x[k].get(h[k]);
+        }
+        if constexpr (kAhead) load(at + step);  // the next row's loads fly during this row's sums
         if (a.post.p) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s = __builtin_fmaf(own.once(e, v[e]), v[e], s);
+            for (int k = 0; k < G; ++k)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s = __builtin_fmaf(own[k].once(e, v[k][e]), v[k][e], s);
             s = team_sum<W>(s, red[0]);
             const float r1 = 1.0f / __builtin_sqrtf(s * inv_cols + a.eps);
             if (live && lane == 0 && a.r_post) a.r_post[row] = r1;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= r1 * post[e];
+            for (int k = 0; k < G; ++k)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[k][e] *= r1 * post[k][e];
         } else if (W > 1) {
             __syncthreads();  // the one sum's array is written again in the next round
         }
         s = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            h[e] = __builtin_fmaf(gate[e], v[e], a.residual_scale * h[e]);
-            s = __builtin_fmaf(own.once(e, h[e]), h[e], s);
+        for (int k = 0; k < G; ++k) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                h[k][e] = __builtin_fmaf(gate[k][e], v[k][e], a.residual_scale * h[k][e]);
+                s = __builtin_fmaf(own[k].once(e, h[k][e]), h[k][e], s);
+            }
+            if (a.h && live) own[k].store((T *)a.h + row * a.ldh, h[k]);
         }
-        if (a.h && live) own.store((T *)a.h + row * a.ldh, h);
         if (!a.y) {
             if (W > 1) __syncthreads();  // as above
             continue;
@@ -160,29 +184,33 @@ __global__ __launch_bounds__(W > 8 ? 64 * W : 512) void residual_norm_kernel(con
         s = team_sum<W>(s, red[1]);
         const float r2 = 1.0f / __builtin_sqrtf(s * inv_cols + a.eps);
         if (live && lane == 0 && a.r_pre) a.r_pre[row] = r2;
-        float y[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = h[e] * r2 * pre[e];
-        if constexpr (!Y8) {
-            if (live) own.store((T *)a.y + row * a.ldy, y);
-        } else {
-            using F = Fp8<false>;
-            // a block is sixteen lanes' groups (bf16), or thirty-two lanes' halves of theirs (fp32)
-            float inv[8];
-            constexpr int kRun = Group<T, RAG>::kRun, kLanes = kBlock8 / kRun;
+        for (int k = 0; k < G; ++k) {
+            float y[8];
 #pragma unroll
-            for (int r = 0; r < 8; r += kRun) {
-                uint32_t m = 0;
+            for (int e = 0; e < 8; ++e) y[e] = h[k][e] * r2 * pre[k][e];
+            if constexpr (!Y8) {
+                if (live) own[k].store((T *)a.y + row * a.ldy, y);
+            } else {
+                using F = Fp8<false>;
+                // a block is sixteen lanes' groups (bf16), or thirty-two lanes' halves of theirs (fp32)
+                float inv[8];
+                constexpr int kRun = Own::kRun, kLanes = kBlock8 / kRun;
 #pragma unroll
-                for (int e = r; e < r + kRun; ++e) m = max(m, magnitude(own.in(e) ? own.once(e, y[e]) : 0.f));
-                const float q = F::scale(group_max_u32<kLanes>(m));
+                for (int r = 0; r < 8; r += kRun) {
+                    uint32_t m = 0;
 #pragma unroll
-                for (int e = r; e < r + kRun; ++e) inv[e] = 1.0f / q;
-                if (live && lane % kLanes == 0 && own.in(r)) a.y_scales[row * a.lds + (lane + r / kRun * kThreads) / kLanes] = q;
+                    for (int e = r; e < r + kRun; ++e) m = max(m, magnitude(own[k].in(e) ? own[k].once(e, y[e]) : 0.f));
+                    const float q = F::scale(group_max_u32<kLanes>(m));
+#pragma unroll
+                    for (int e = r; e < r + kRun; ++e) inv[e] = 1.0f / q;
+                    if (live && lane % kLanes == 0 && own[k].in(r))
+                        a.y_scales[row * a.lds + (lane + (k * Own::kRuns + r / kRun) * kThreads) / kLanes] = q;
+                }
+                const uint32_t w[2] = {F::pack(y[0] * inv[0], y[1] * inv[1], y[2] * inv[2], y[3] * inv[3]),
+                                       F::pack(y[4] * inv[4], y[5] * inv[5], y[6] * inv[6], y[7] * inv[7])};
+                if (live) own[k].store_bytes((uint8_t *)a.y + row * a.ldy, w);
             }
-            const uint32_t w[2] = {F::pack(y[0] * inv[0], y[1] * inv[1], y[2] * inv[2], y[3] * inv[3]),
-                                   F::pack(y[4] * inv[4], y[5] * inv[5], y[6] * inv[6], y[7] * inv[7])};
-            if (live) own.store_bytes((uint8_t *)a.y + row * a.ldy, w);
         }
     }
 }
@@ -301,53 +329,84 @@ __device__ __forceinline__ float *gate_slot(const GradArgs &a, int64_t run, bool
 // groups lie in LDS, every lane's own where it alone reads them: a lane has 128 registers.  Of the
 // three sums over rows two grow by the row, dy hn and H un: while the gate is the same, dgate is gamma_post times the latter
 // and dgamma_post the gate times it.
-template <typename T, int W, bool RAG>
+// With two groups of eight to a lane (G) there is no LDS left for the sum by groups, which lies in the workspace then.
+template <typename T, int W, int G, bool RAG>
 __global__ __launch_bounds__(1024) void residual_norm_grad_kernel(const GradArgs a)
 {
     constexpr int kWaves = 16, kTeams = kWaves / W, kThreads = 64 * W, kAll = 64 * kWaves;
-    enum { kPre, kGatePost, kSumPost, kPlanes };
+    enum { kPre, kGatePost, kSumPost, kPlanes = G == 1 ? 3 : 2 };
+    constexpr bool kAhead = G == 1;  // (two groups leave no registers for the next row's operands)
+    constexpr bool kTwice = G * sizeof(T) > 4;  // (... of fp32, none for u from one sum to the next: it is read again)
     __shared__ float red[2][kWaves];
-    __shared__ float4_t own[kPlanes][2][kAll];
+    __shared__ float4_t own[kPlanes][G][2][kAll];
     const int tid = threadIdx.x, team = __builtin_amdgcn_readfirstlane(tid >> 6) / W, lane = tid - team * kThreads;
     const float inv_cols = 1.0f / (float)a.cols;
     const bool has_post = a.post.p != nullptr, has_gate = a.gate.p != nullptr;
-    Group<T, RAG> here(lane, kThreads, a.cols);
-    auto get_own = [&](int which, int q, float (&v)[4]) {
-        const float4_t f = own[which][q][tid];
+    using Own = Group<T, RAG>;
+    Own here[G];
+#pragma unroll
+    for (int k = 0; k < G; ++k) here[k] = Own(lane + k * Own::kRuns * kThreads, kThreads, a.cols);
+    auto get_own = [&](int which, int k, int q, float (&v)[4]) {
+        const float4_t f = own[which][k][q][tid];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = f[e];
     };
-    auto put_own = [&](int which, const float (&v)[8]) {
-        own[which][0][tid] = float4_t{v[0], v[1], v[2], v[3]};
-        own[which][1][tid] = float4_t{v[4], v[5], v[6], v[7]};
+    auto put_own = [&](int which, int k, const float (&v)[8]) {
+        own[which][k][0][tid] = float4_t{v[0], v[1], v[2], v[3]};
+        own[which][k][1][tid] = float4_t{v[4], v[5], v[6], v[7]};
     };
-    float sum_pre[8], sum_un[8], v8[8];
+    // the sum by groups, of the lane's own columns
+    float *const posts = a.ws + ((int64_t)a.runs + blockIdx.x) * a.cols;
+    auto get_sum_post = [&](int k, float (&v)[8]) {
+        if constexpr (G == 1) {
+            float lo[4], hi[4];
+            get_own(kSumPost, 0, 0, lo), get_own(kSumPost, 0, 1, hi);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum_pre[e] = v8[e] = 0.f;
+            for (int e = 0; e < 4; ++e) v[e] = lo[e], v[4 + e] = hi[e];
+        } else {
+            here[k].load_as(posts, v);
+        }
+    };
+    auto put_sum_post = [&](int k, const float (&v)[8]) {
+        if constexpr (G == 1)
+            put_own(kSumPost, 0, v);
+        else
+            here[k].store_cached(posts, v);
+    };
+    float sum_pre[G][8], sum_un[G][8], v8[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        v8[e] = 0.f;
+#pragma unroll
+        for (int k = 0; k < G; ++k) sum_pre[k][e] = 0.f;
+    }
     // gamma_post, or one, or the gate of group g, or one
-    auto get_post = [&](float (&v)[8]) {
+    auto get_post = [&](int k, float (&v)[8]) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = 1.f;
-        if (has_post) a.post.group(0, here, v);
+        if (has_post) a.post.group(0, here[k], v);
     };
-    auto get_gate = [&](int g, float (&v)[8]) {
+    auto get_gate = [&](int g, int k, float (&v)[8]) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = 1.f;
-        if (has_gate) a.gate.group((int64_t)g * a.ldg, here, v);
+        if (has_gate) a.gate.group((int64_t)g * a.ldg, here[k], v);
     };
-    const bool all_in = a.cols == 8 * kThreads && a.has_dy && a.has_dh;
+    const bool all_in = a.cols == 8 * G * kThreads && a.has_dy && a.has_dh;
 
-    Eight<T> next_dy, next_dh, next_h, next_u;
+    Eight<T> next_dy[G], next_dh[G], next_h[G], next_u[G];
     float next_r2, next_r1;
     auto load = [&](int to) {
         const int64_t r = min(to, a.rows - 1);
-        // (a new value to the compiler for each row: it would keep a 64-bit address for every operand and lane otherwise)
-        asm volatile("" : "+v"(here.at[0]));
-        if constexpr (here.kRuns > 1) asm volatile("" : "+v"(here.at[1]));
-        here.load(next_dy, (const T *)a.dy + r * a.lddy);
-        here.load(next_h, (const T *)a.h + r * a.ldh);
-        here.load(next_dh, (const T *)a.dh + r * a.lddh);
-        here.load(next_u, (const T *)a.u + r * a.ldu);
+#pragma unroll
+        for (int k = 0; k < G; ++k) {
+            // (a new value to the compiler for each row: it would keep a 64-bit address for every operand and lane otherwise)
+            asm volatile("" : "+v"(here[k].at[0]));
+            if constexpr (Own::kRuns > 1) asm volatile("" : "+v"(here[k].at[1]));
+            here[k].load(next_dy[k], (const T *)a.dy + r * a.lddy);
+            here[k].load(next_h[k], (const T *)a.h + r * a.ldh);
+            here[k].load(next_dh[k], (const T *)a.dh + r * a.lddh);
+            here[k].load(next_u[k], (const T *)a.u + r * a.ldu);
+        }
         // (not given: some other number, not used)
         next_r2 = *(a.has_dy ? a.r_pre + r : a.ws), next_r1 = *(has_post ? a.r_post + r : a.ws);
     };
@@ -361,30 +420,42 @@ __global__ __launch_bounds__(1024) void residual_norm_grad_kernel(const GradArgs
     int g = div_by(begin, per, a.gate_magic) + (each ? team : 0);  // the group of rows whose gate is in use
     int row = each ? g * per : (spread ? blockIdx.x * kTeams : begin) + team;
     int from = begin;  // the round's first row, the same for all teams
-    load(row);  // (ahead of the parameters: both fly together)
-    put_own(kSumPost, v8);
-    if (a.has_dy) a.pre.group(0, here, v8);
-    put_own(kPre, v8);
+    if constexpr (kAhead) load(row);  // (ahead of the parameters: both fly together)
+#pragma unroll
+    for (int k = 0; k < G; ++k) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v8[e] = 0.f;
+        if (a.dpost) put_sum_post(k, v8);
+        if (a.has_dy) a.pre.group(0, here[k], v8);
+        put_own(kPre, k, v8);
+    }
 
     // one row of this team (a dead one adds nothing and writes nothing); `next` is loaded meanwhile
     auto one = [&](int64_t row, bool live, int next) {
+        if constexpr (!kAhead) load((int)row);
         const float r2 = a.has_dy && live ? next_r2 : 0.f, r1 = !has_post ? 1.f : live ? next_r1 : 0.f;
-        Eight<T> dy = next_dy, h = next_h, dh = next_dh, u = next_u;
-        if (!(live && all_in)) {
-            here.keep(dy, live && a.has_dy), here.keep(h, live && a.has_dy), here.keep(dh, live && a.has_dh), here.keep(u, live);
+        Eight<T> dy[G], h[G], dh[G], u[G];
+#pragma unroll
+        for (int k = 0; k < G; ++k) {
+            dy[k] = next_dy[k], h[k] = next_h[k], dh[k] = next_dh[k], u[k] = next_u[k];
+            if (!(live && all_in)) {
+                here[k].keep(dy[k], live && a.has_dy), here[k].keep(h[k], live && a.has_dy);
+                here[k].keep(dh[k], live && a.has_dh), here[k].keep(u[k], live);
+            }
         }
-        load(next);
+        if constexpr (kAhead) load(next);
         float s = 0.f;
         if (a.has_dy) {
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
+            for (int p = 0; p < 2 * G; ++p) {
+                const int k = p >> 1, q = p & 1;
                 float t[4], hv[4], pre[4];
-                dy.get_half(q, t), h.get_half(q, hv), get_own(kPre, q, pre);
+                dy[k].get_half(q, t), h[k].get_half(q, hv), get_own(kPre, k, q, pre);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float th = t[e] * hv[e];
-                    sum_pre[4 * q + e] = __builtin_fmaf(th, r2, sum_pre[4 * q + e]);
-                    s = __builtin_fmaf(here.once(4 * q + e, th), pre[e], s);
+                    sum_pre[k][4 * q + e] = __builtin_fmaf(th, r2, sum_pre[k][4 * q + e]);
+                    s = __builtin_fmaf(here[k].once(4 * q + e, th), pre[e], s);
                 }
                 __builtin_amdgcn_sched_barrier(0);  // (reads of the next half's operands ahead of here cost registers)
             }
@@ -393,48 +464,61 @@ __global__ __launch_bounds__(1024) void residual_norm_grad_kernel(const GradArgs
             __syncthreads();  // the one sum's array is written again in the next row
         }
         const float of_h = -r2 * r2 * (r2 * s * inv_cols);  // H = dh + r2 t - r2 hn mean(t hn)
-        dy.renew(), h.renew();
         s = 0.f;
-        float v[8], dx[8];
+        float v[G][8];
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            float t[4], hv[4], H[4], pre[4], un[4], gp[4];
-            dy.get_half(q, t), h.get_half(q, hv), dh.get_half(q, H), u.get_half(q, un);
-            get_own(kPre, q, pre), get_own(kGatePost, q, gp);
+        for (int k = 0; k < G; ++k) {
+            dy[k].renew(), h[k].renew();
+            float dx[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                H[e] = __builtin_fmaf(hv[e], of_h, __builtin_fmaf(t[e] * pre[e], r2, H[e]));
-                un[e] *= r1;
-                sum_un[4 * q + e] = __builtin_fmaf(H[e], un[e], sum_un[4 * q + e]);
-                v[4 * q + e] = H[e] * gp[e];
-                s = __builtin_fmaf(here.once(4 * q + e, v[4 * q + e]), un[e], s);
-                dx[4 * q + e] = a.residual_scale * H[e];
+            for (int q = 0; q < 2; ++q) {
+                float t[4], hv[4], H[4], pre[4], un[4], gp[4];
+                dy[k].get_half(q, t), h[k].get_half(q, hv), dh[k].get_half(q, H), u[k].get_half(q, un);
+                get_own(kPre, k, q, pre), get_own(kGatePost, k, q, gp);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    H[e] = __builtin_fmaf(hv[e], of_h, __builtin_fmaf(t[e] * pre[e], r2, H[e]));
+                    un[e] *= r1;
+                    sum_un[k][4 * q + e] = __builtin_fmaf(H[e], un[e], sum_un[k][4 * q + e]);
+                    v[k][4 * q + e] = H[e] * gp[e];
+                    s = __builtin_fmaf(here[k].once(4 * q + e, v[k][4 * q + e]), un[e], s);
+                    dx[4 * q + e] = a.residual_scale * H[e];
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
-            __builtin_amdgcn_sched_barrier(0);
+            if (live) here[k].store((T *)a.dx + row * a.lddx, dx);
         }
-        if (live) here.store((T *)a.dx + row * a.lddx, dx);
         if (has_post) {
             const float of_u = -r1 * r1 * (team_sum<W>(s, red[1]) * inv_cols);  // du = r1 v - r1 un mean(v un)
-            u.renew();
-            float uv[8];
-            u.get(uv);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(uv[e], of_u, r1 * v[e]);
+            for (int k = 0; k < G; ++k) {
+                if constexpr (kTwice)
+                    here[k].load(u[k], (const T *)a.u + min((int)row, a.rows - 1) * a.ldu);
+                else
+                    u[k].renew();
+                float uv[8];
+                u[k].get(uv);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[k][e] = __builtin_fmaf(uv[e], of_u, r1 * v[k][e]);
+            }
         } else if (W > 1) {
             __syncthreads();  // as above
         }
-        if (live) here.store((T *)a.du + row * a.lddu, v);
+        if (live) {
+#pragma unroll
+            for (int k = 0; k < G; ++k) here[k].store((T *)a.du + row * a.lddu, v[k]);
+        }
     };
     // the teams' sums v, added in the teams' order: the first team has them.  The gate's place serves, until the next one comes
     auto join = [&](float (&v)[8]) {
-        if constexpr (kTeams > 1) {
+        if constexpr (kTeams > 1) {  // (one group a lane)
             __syncthreads();
-            put_own(kGatePost, v);
+            put_own(kGatePost, 0, v);
             __syncthreads();
             if (team == 0) {
                 for (int o = 1; o < kTeams; ++o)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] += own[kGatePost][e >> 2][o * kThreads + lane][e & 3];
+                    for (int e = 0; e < 8; ++e) v[e] += own[kGatePost][0][e >> 2][o * kThreads + lane][e & 3];
             }
             __syncthreads();
         }
@@ -442,55 +526,61 @@ __global__ __launch_bounds__(1024) void residual_norm_grad_kernel(const GradArgs
 
     while (from < end) {
         const int stop = spread ? a.rows : min(end, (g + 1) * per), first = spread ? blockIdx.x * kTeams : from;
-        if (g * per < end) {
-            float gate[8];
-            get_gate(g, gate), get_post(v8);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v8[e] *= gate[e];
-            put_own(kGatePost, v8);
+        for (int k = 0; k < G; ++k) {
+            if (g * per < end) {
+                float gate[8];
+                get_gate(g, k, gate), get_post(k, v8);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v8[e] *= gate[e];
+                put_own(kGatePost, k, v8);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum_un[k][e] = 0.f;
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum_un[e] = 0.f;
         const int rounds = each ? per : (stop - first + step - 1) / step;
         for (int i = rounds; i > 0; --i) {
             const int next = each ? (i > 1 ? row + 1 : (g + kTeams) * per) : (i > 1 ? row + step : stop + team);
             one(row, row < stop, next);
             row = next;
         }
-if (a.dpost && g * per < end) {
-            float lo[4], hi[4];
-            get_gate(g, v8), get_own(kSumPost, 0, lo), get_own(kSumPost, 1, hi);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v8[e] = __builtin_fmaf(v8[e], sum_un[e], e < 4 ? lo[e & 3] : hi[e & 3]);
-            put_own(kSumPost, v8);
-        }
-        if (a.dgate.p) {
-            if (!each) join(sum_un);
-            const bool begins = g * per >= begin, ends = min(a.rows, (g + 1) * per) <= end;
-            if (each ? g * per < end : team == 0) {
-                get_post(v8);
+        for (int k = 0; k < G; ++k) {
+            if (a.dpost && g * per < end) {
+                float sum[8];
+                get_gate(g, k, v8), get_sum_post(k, sum);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum_un[e] *= v8[e];
-                if (begins && ends)
-                    a.dgate.put_group((int64_t)g * a.lddg, here, sum_un);
-                else
-                    here.store(gate_slot(a, blockIdx.x, begins), sum_un);
+                for (int e = 0; e < 8; ++e) sum[e] = __builtin_fmaf(v8[e], sum_un[k][e], sum[e]);
+                put_sum_post(k, sum);
+            }
+            if (a.dgate.p) {
+                if (!each) join(sum_un[k]);
+                const bool begins = g * per >= begin, ends = min(a.rows, (g + 1) * per) <= end;
+                if (each ? g * per < end : team == 0) {
+                    get_post(k, v8);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum_un[k][e] *= v8[e];
+                    if (begins && ends)
+                        a.dgate.put_group((int64_t)g * a.lddg, here[k], sum_un[k]);
+                    else
+                        here[k].store(gate_slot(a, blockIdx.x, begins), sum_un[k]);
+                }
             }
         }
         g += each ? kTeams : 1;
         from = each ? (g - team) * per : stop;
     }
-    if (a.dpre && a.has_dy) {
-        join(sum_pre);
-        if (team == 0) here.store(a.ws + (int64_t)blockIdx.x * a.cols, sum_pre);
-    }
-    if (a.dpost) {
-        float lo[4], hi[4];
-        get_own(kSumPost, 0, lo), get_own(kSumPost, 1, hi);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v8[e] = lo[e], v8[4 + e] = hi[e];
-        join(v8);
-        if (team == 0) here.store(a.ws + ((int64_t)a.runs + blockIdx.x) * a.cols, v8);
+    for (int k = 0; k < G; ++k) {
+        if (a.dpre && a.has_dy) {
+            join(sum_pre[k]);
+            if (team == 0) here[k].store(a.ws + (int64_t)blockIdx.x * a.cols, sum_pre[k]);
+        }
+        if (a.dpost && G == 1) {
+            get_sum_post(k, v8);
+            join(v8);
+            if (team == 0) here[k].store(posts, v8);
+        }
     }
 }
 
@@ -625,24 +715,26 @@ __global__ __launch_bounds__(256) void residual_norm_grad_cols_kernel(const Grad
 
 // ---- entry points --------------------------------------------------------------------------------------------------
 // columns of the kernels that hold a row: a group of eight, and what 16 waves have room for
-constexpr int kNarrowest = 8, kWidest = 16 * 64 * 8;
+constexpr int kNarrowest = 8, kWidest = 16 * 64 * 8 * 2;
 inline bool row_fits(int64_t cols) { return cols >= kNarrowest && cols <= kWidest; }
 
-// f(waves of a team) for rows that fit one
+// f(waves of a team, groups of eight to a lane) for rows that fit one
 template <typename F>
 static void with_team(int64_t cols, F &&f)
 {
     using std::integral_constant;
     if (cols <= 512)
-        f(integral_constant<int, 1>{});
+        f(integral_constant<int, 1>{}, integral_constant<int, 1>{});
     else if (cols <= 1024)
-        f(integral_constant<int, 2>{});
+        f(integral_constant<int, 2>{}, integral_constant<int, 1>{});
     else if (cols <= 2048)
-        f(integral_constant<int, 4>{});
+        f(integral_constant<int, 4>{}, integral_constant<int, 1>{});
     else if (cols <= 4096)
-        f(integral_constant<int, 8>{});
+        f(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+    else if (cols <= 8192)
+        f(integral_constant<int, 16>{}, integral_constant<int, 1>{});
     else
-        f(integral_constant<int, 16>{});
+        f(integral_constant<int, 16>{}, integral_constant<int, 2>{});
 }
 
 template <typename T, bool Y8>
@@ -652,17 +744,17 @@ static void launch_norm(const NormArgs &a, hipStream_t stream)
         residual_norm_any_kernel<T, Y8><<<(unsigned)std::min<int64_t>(a.rows, 65536), 1024, 0, stream>>>(a);
         return;
     }
-    with_team(a.cols, [&](auto w) {
-        constexpr int W = w, kTeams = W > 8 ? 1 : 8 / W, kThreads = W > 8 ? 1024 : 512;
+    with_team(a.cols, [&](auto w, auto groups) {
+        constexpr int W = w, G = groups, kTeams = W > 8 ? 1 : 8 / W, kThreads = W > 8 ? 1024 : 512;
         // One workgroup per CU: more of them read more places of memory at once (8192 x 4096 bf16: 46.7 us with 256, 48.5 with
         // 512, 53 with 1024).  A gate that changes after a few rows is waited for, which a second one hides (of every element's
         // own: 56 us with 512, 79 with 256).
         const int64_t most = a.gate.p && a.gate_rows < 16 ? 512 : 256;
         const int64_t grid = std::min<int64_t>((a.rows + kTeams - 1) / kTeams, most);
         if (a.cols % 8)
-            residual_norm_kernel<T, W, Y8, true><<<(unsigned)grid, kThreads, 0, stream>>>(a);
+            residual_norm_kernel<T, W, G, Y8, true><<<(unsigned)grid, kThreads, 0, stream>>>(a);
         else
-            residual_norm_kernel<T, W, Y8, false><<<(unsigned)grid, kThreads, 0, stream>>>(a);
+            residual_norm_kernel<T, W, G, Y8, false><<<(unsigned)grid, kThreads, 0, stream>>>(a);
     });
 }
 
@@ -693,12 +785,12 @@ static void launch_grad(GradArgs a, hipStream_t stream)
         residual_norm_grad_cols_kernel<T><<<dim3((a.cols + 255) / 256, a.runs), 256, 0, stream>>>(a, means);
         residual_norm_grad_any_kernel<T, false><<<grid, 1024, 0, stream>>>(a, means);
     } else {
-        with_team(a.cols, [&](auto w) {
-            constexpr int W = w;
+        with_team(a.cols, [&](auto w, auto groups) {
+            constexpr int W = w, G = groups;
             if (a.cols % 8)
-                residual_norm_grad_kernel<T, W, true><<<a.runs, 1024, 0, stream>>>(a);
+                residual_norm_grad_kernel<T, W, G, true><<<a.runs, 1024, 0, stream>>>(a);
             else
-                residual_norm_grad_kernel<T, W, false><<<a.runs, 1024, 0, stream>>>(a);
+                residual_norm_grad_kernel<T, W, G, false><<<a.runs, 1024, 0, stream>>>(a);
         });
     }
     // (a gate whose groups lie within runs has its sums already)
