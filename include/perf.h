@@ -244,7 +244,9 @@ perf_status perf_quantize_fp8(const void *x, void *q, float *scales, void *qt, f
 /* Product of block-scaled 8-bit matrices, dense or batched, the 8-bit form of perf_gemm with A row-major and B column-major:
  *     C_b[m][n] = alpha * sum over blocks j of 128 of K:
  *                     scaleA_b[m][j] * scaleB_b[n / b_block_rows][j] * sum_{k in block j} A_b[m][k] * B_b[n][k],
- * products and sums in fp32, one rounding to c_dt.
+ * one rounding to c_dt.  Sums are fp32.  For f32 C every product is exact; for bf16 C the matrix instructions, of eight
+ * products that they add at once, drop what lies below 2^-13 of the largest (less than 2^-10 of the sum of the products'
+ * magnitudes in the worst case, 1e-5 to 4e-5 of C as a rule, where a rounding to bf16 is 4e-3).
  *   A       device, M x K, 8-bit, row stride lda; a_dt E4M3 or E5M2;  scaleA  device fp32, M x ceil(K/128), row stride ldsa
  *   B       device, N x K, 8-bit, row stride ldb; b_dt E4M3;  scaleB  device fp32, ceil(N / b_block_rows) x ceil(K/128), row
  *           stride ldsb; b_block_rows 1 (a scale for 128 elements of a row) or 128 (for a tile)
@@ -252,8 +254,9 @@ perf_status perf_quantize_fp8(const void *x, void *q, float *scales, void *qt, f
  *   batch   as in perf_gemm: matrix b starts stride* elements after matrix b-1 (strideSA and strideSB in scales)
  * The last block may be short; what lies in memory behind a row's K elements is not used.
  * Errors: NULL, SHAPE (dimension < 1 or > 2^30, ld too small, negative stride, batches overlapping in C, b_block_rows not 1
- * or 128), DTYPE, ALIGN (A or B not 16-byte aligned, scales or C not aligned to their elements), UNSUPPORTED (b_dt E5M2; lda,
- * ldb, strideA or strideB not a multiple of 16, or a row stride of A, B or their scales of 2^23 or more), LAUNCH. */
+ * or 128, alpha not finite), DTYPE, ALIGN (A or B not 16-byte aligned, scales or C not aligned to their elements),
+ * UNSUPPORTED (b_dt E5M2; lda, ldb, strideA or strideB not a multiple of 16; a row stride of A, B or their scales of 2^23 or
+ * more; more tiles of C, of 128 x 128, than a launch holds), LAUNCH. */
 perf_status perf_gemm_fp8(const void *A, const float *scaleA, const void *B, const float *scaleB, void *C, int64_t M, int64_t N,
                           int64_t K, int64_t lda, int64_t ldsa, int64_t ldb, int64_t ldsb, int64_t ldc, int64_t b_block_rows,
                           int64_t batch, int64_t strideA, int64_t strideSA, int64_t strideB, int64_t strideSB, int64_t strideC,

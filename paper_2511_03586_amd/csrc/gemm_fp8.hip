@@ -642,7 +642,11 @@ static perf_status gemm8(const Gemm8Args &g, hipStream_t stream)
     // A tile kernel on less than the whole chip begins sooner, the waves that divide K then go on faster.  128 tiles: K = 1024
     // 8.8 us against 12.7, K = 4096 26.7 against 23.3 (bf16 C); K = 700 13.0 against 14.1, K = 4096 42 against 29.5 (fp32 C).
     // 256 tiles, K = 4096: 28.5 against 36 (bf16), 45 against 54 (fp32).  64 tiles, K = 8192: 47 against 20.
-    if (mid >= 200 || (mid >= 100 && blocks <= (WIDE ? 8 : 20))) return launch_tile<4, 4, 2, 2, A5, CT>(g, stream);
+    // Few rows leave a tile part empty: 256 tiles of 32 rows, K = 4096 41 against 33 (fp32 50 against 33), 512 of them, K = 1024 15.4
+    // against 21; 128 of 64 rows, K = 2048 15.5 against 10.8, 256 of them 17.4 against 20.
+    // (and a launch of the waves, whose tiles are smaller, does not hold 2^29 columns)
+    const bool tiles = mid >= 200 ? g.M > 32 || blocks <= 8 || mid > (1 << 20) : mid >= 100 && g.M > 64 && blocks <= (WIDE ? 8 : 20);
+    if (tiles) return launch_tile<4, 4, 2, 2, A5, CT>(g, stream);
     if (g.M <= 16) return waves_by_columns<1, A5, CT>(g, stream);
     if (g.M <= 32) return waves_by_columns<2, A5, CT>(g, stream);
     return waves_by_columns<4, A5, CT>(g, stream);
@@ -663,7 +667,12 @@ extern "C" perf_status perf_gemm_fp8(const void *A, const float *scaleA, const v
     if (lda < K || ldb < K || ldsa < blocks || ldsb < blocks || ldc < N) return PERF_ERR_SHAPE;
     if (b_block_rows != 1 && b_block_rows != kBlock8) return PERF_ERR_SHAPE;
     if (strideA < 0 || strideSA < 0 || strideB < 0 || strideSB < 0 || strideC < 0) return PERF_ERR_SHAPE;
-    if (batch > 1 && strideC < (M - 1) * ldc + N) return PERF_ERR_SHAPE;
+    if (!addressable(M, lda) || !addressable(N, ldb) || !addressable(M, ldsa) || !addressable(N, ldsb) || !addressable(M, ldc))
+        return PERF_ERR_SHAPE;
+    if (batch > 1 && (!addressable(batch, strideA) || !addressable(batch, strideSA) || !addressable(batch, strideB) ||
+                      !addressable(batch, strideSB) || !addressable(batch, strideC) || strideC < (M - 1) * ldc + N))
+        return PERF_ERR_SHAPE;
+    if (!std::isfinite(alpha)) return PERF_ERR_SHAPE;
     if (!dtype8_ok(a_dt) || !dtype8_ok(b_dt) || !dtype_ok(c_dt)) return PERF_ERR_DTYPE;
     if (!aligned(A, 16) || !aligned(B, 16) || !aligned(scaleA, 4) || !aligned(scaleB, 4) || !aligned(C, dtype_size(c_dt)))
         return PERF_ERR_ALIGN;

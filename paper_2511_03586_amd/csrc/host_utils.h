@@ -26,5 +26,7 @@ constexpr int64_t max_blocks(int threads) { return 4294967295LL / threads; }
 
 // Extents of the operators on 8-bit values: indexes of rows, columns and blocks are 32 bits wide in their kernels.
 constexpr int64_t kMaxExtent8 = 1ll << 30;
+// whether the bytes of `rows` rows, `ld` elements apart, have offsets of 63 bits
+inline bool addressable(int64_t rows, int64_t ld) { return ld <= INT64_MAX / 8 / rows; }
 
 }  // namespace perf

@@ -363,6 +363,9 @@ extern "C" perf_status perf_quantize_fp8(const void *x, void *q, float *scales, 
     const int64_t row_blocks = (rows + kBlock8 - 1) / kBlock8, col_blocks = (cols + kBlock8 - 1) / kBlock8;
     if (q && (ldq < cols || lds < col_blocks)) return PERF_ERR_SHAPE;
     if (qt && (ldqt < rows || ldst < row_blocks)) return PERF_ERR_SHAPE;
+    if (!addressable(rows, ldx) || (q && (!addressable(rows, ldq) || !addressable(rows, lds))) ||
+        (qt && (!addressable(cols, ldqt) || !addressable(cols, ldst))))
+        return PERF_ERR_SHAPE;
     if (!dtype_ok(x_dt) || !dtype8_ok(q_dt)) return PERF_ERR_DTYPE;
     if (!aligned(x, dtype_size(x_dt)) || !aligned(scales, 4) || !aligned(scales_t, 4)) return PERF_ERR_ALIGN;
     const QuantizeArgs a{x, (uint8_t *)q, (uint8_t *)qt, scales, scales_t, rows, cols, ldx, ldq, lds, ldqt, ldst, (hipStream_t)stream};

@@ -815,7 +815,10 @@ extern "C" perf_status perf_residual_norm(const void *u, const void *x, const vo
     if (rows < 1 || cols < 1 || rows > kMaxExtent8 || cols > kMaxExtent8 || ldu < cols || ldx < cols || (h && ldh < cols) || (y && ldy < cols))
         return PERF_ERR_SHAPE;
     if (gate && (ldg < cols || gate_rows < 1)) return PERF_ERR_SHAPE;
-    if (y8 && lds < (cols + kBlock8 - 1) / kBlock8) return PERF_ERR_SHAPE;
+    if (y8 && (lds < (cols + kBlock8 - 1) / kBlock8 || !addressable(rows, lds))) return PERF_ERR_SHAPE;
+    if (!addressable(rows, ldu) || !addressable(rows, ldx) || (h && !addressable(rows, ldh)) || (y && !addressable(rows, ldy)) ||
+        (gate && !addressable(rows, ldg)))
+        return PERF_ERR_SHAPE;
     if (!(eps >= 0.f) || !std::isfinite(eps) || !std::isfinite(residual_scale)) return PERF_ERR_SHAPE;
     if (!dtype_ok(x_dt) || !dtype_ok(param_dt) || (gate && !dtype_ok(gate_dt)) || (y && !dtype_ok(y_dt) && !dtype8_ok(y_dt)))
         return PERF_ERR_DTYPE;
@@ -868,6 +871,9 @@ extern "C" perf_status perf_residual_norm_backward(const void *dy, const void *d
         lddx < cols || lddu < cols)
         return PERF_ERR_SHAPE;
     if (gate && (ldg < cols || gate_rows < 1 || (dgate && lddg < cols))) return PERF_ERR_SHAPE;
+    if ((dy && (!addressable(rows, lddy) || !addressable(rows, ldh))) || (dh && !addressable(rows, lddh)) || !addressable(rows, ldu) ||
+        !addressable(rows, lddx) || !addressable(rows, lddu) || (gate && !addressable(rows, ldg)) || (dgate && !addressable(rows, lddg)))
+        return PERF_ERR_SHAPE;
     if (!std::isfinite(residual_scale)) return PERF_ERR_SHAPE;
     if (!dtype_ok(x_dt) || !dtype_ok(param_dt) || (gate && !dtype_ok(gate_dt))) return PERF_ERR_DTYPE;
     const int64_t sz = dtype_size(x_dt), psz = dtype_size(param_dt), gsz = gate ? dtype_size(gate_dt) : 1;
