@@ -355,8 +355,10 @@ __global__ __launch_bounds__(1024) void residual_norm_grad_kernel(const GradArgs
         own[which][k][0][tid] = float4_t{v[0], v[1], v[2], v[3]};
         own[which][k][1][tid] = float4_t{v[4], v[5], v[6], v[7]};
     };
-    // the sum by groups, of the lane's own columns
-    float *const posts = a.ws + ((int64_t)a.runs + blockIdx.x) * a.cols;
+    // the sums of this run, of which a single one has the results; posts grows by groups, each lane its own columns
+    const bool only = a.runs == 1;
+    float *const pres = only ? a.dpre : a.ws + (int64_t)blockIdx.x * a.cols;
+    float *const posts = only ? a.dpost : a.ws + ((int64_t)a.runs + blockIdx.x) * a.cols;
     auto get_sum_post = [&](int k, float (&v)[8]) {
         if constexpr (G == 1) {
             float lo[4], hi[4];
@@ -574,7 +576,7 @@ __global__ __launch_bounds__(1024) void residual_norm_grad_kernel(const GradArgs
     for (int k = 0; k < G; ++k) {
         if (a.dpre && a.has_dy) {
             join(sum_pre[k]);
-            if (team == 0) here[k].store(a.ws + (int64_t)blockIdx.x * a.cols, sum_pre[k]);
+            if (team == 0) here[k].store(pres, sum_pre[k]);
         }
         if (a.dpost && G == 1) {
             get_sum_post(k, v8);
@@ -584,46 +586,52 @@ __global__ __launch_bounds__(1024) void residual_norm_grad_kernel(const GradArgs
     }
 }
 
-// The runs' sums, added in the order of the rows.  blockIdx.y: 0 = dgamma_pre, 1 = dgamma_post, then the gates of groups that
-// begin in one run and go on beyond it: by group, or (by_run) by the run in which it begins, whichever are fewer.  64 columns
-// and sixteen parts of the runs per workgroup, the parts added in order.
-__global__ __launch_bounds__(1024) void residual_norm_sums_kernel(const GradArgs a, bool by_run)
+// The runs' sums, added in the order of the rows, 64 columns per workgroup.  blockIdx.y: 0 = dgamma_pre, 1 = dgamma_post, sixteen
+// parts of the runs side by side; then the gates of groups that begin in one run and go on beyond it, by group or (by_run) by
+// the run in which it begins, whichever are fewer: one gate in sixteen parts, or sixteen gates (each_part) of few runs.
+__global__ __launch_bounds__(1024) void residual_norm_sums_kernel(const GradArgs a, bool by_run, bool each_part, int gates)
 {
     constexpr int kParts = 16;
     __shared__ float parts[kParts][64];
-    const int lane = threadIdx.x & 63, part = threadIdx.x >> 6, col = blockIdx.x * 64 + lane;
-    const int which = blockIdx.y;
+    const int lane = threadIdx.x & 63, part = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = blockIdx.x * 64 + lane;
+    const bool gamma = blockIdx.y < 2, post = blockIdx.y == 1;
+    const int gate = each_part ? (blockIdx.y - 2) * kParts + part : blockIdx.y - 2;
     int count = a.runs, g = 0;
-    const float *from = a.ws + (int64_t)which * a.runs * a.cols;  // the sums of run i lie `step` after those of run i - 1
+    const float *from = a.ws + (post ? (int64_t)a.runs * a.cols : 0);  // the sums of run i lie `step` after those of run i - 1
     int64_t step = a.cols;
-    if (which < 2) {
-        if (!(which ? a.dpost : a.dpre)) return;
-        if (which == 0 && !a.has_dy) count = 0;
+    if (gamma) {
+        if (!(post ? a.dpost : a.dpre)) return;
+        if (!post && !a.has_dy) count = 0;
     } else {
-        g = by_run ? div_by(min(a.rows, (which - 1) * a.run) - 1, a.gate_rows, a.gate_magic) : which - 2;
+        if (gate >= gates) return;  // (whole waves, and no barrier behind)
+        g = by_run ? div_by(min(a.rows, (gate + 1) * a.run) - 1, a.gate_rows, a.gate_magic) : gate;
         const int begin = g * a.gate_rows, end = min(a.rows, begin + a.gate_rows), t = begin / a.run;
-        if ((by_run && t != which - 2) || end <= (t + 1) * a.run) return;
+        if ((by_run && t != gate) || end <= (t + 1) * a.run) return;
         from = gate_slot(a, t, true);  // ... of the first, one row of slots early for the others
         step = 2 * (int64_t)a.cols;
         count = (end - 1) / a.run - t + 1;
     }
-    const int per = (count + kParts - 1) / kParts, lo = part * per, hi = min(count, lo + per);
+    const bool alone = !gamma && each_part;
+    const int per = alone ? count : (count + kParts - 1) / kParts, lo = alone ? 0 : part * per, hi = min(count, lo + per);
     float s = 0.f;
     if (col < a.cols) {
 #pragma unroll 8
-        for (int i = lo; i < hi; ++i) s += from[i * step - (which >= 2 && i > 0 ? a.cols : 0) + col];
+        for (int i = lo; i < hi; ++i) s += from[i * step - (!gamma && i > 0 ? a.cols : 0) + col];
     }
-    parts[part][lane] = s;
-    __syncthreads();
-    if (part || col >= a.cols) return;
+    if (!alone) {
+        parts[part][lane] = s;
+        __syncthreads();
+        if (part) return;
 #pragma unroll
-    for (int p = 1; p < kParts; ++p) s += parts[p][lane];
-    if (which == 0)
-        a.dpre[col] = s;
-    else if (which == 1)
+        for (int p = 1; p < kParts; ++p) s += parts[p][lane];
+    }
+    if (col >= a.cols) return;
+    if (!gamma)
+        a.dgate.put((int64_t)g * a.lddg + col, s);
+    else if (post)
         a.dpost[col] = s;
     else
-        a.dgate.put((int64_t)g * a.lddg + col, s);
+        a.dpre[col] = s;
 }
 
 // Rows of any length, in three kernels: every row's mean(t hn) into the workspace; a lane per column, which computes H
@@ -763,14 +771,21 @@ struct RunPlan {
     int run, runs;
     bool whole_groups;
 };
-// A run for each CU.
-static RunPlan plan_runs(int64_t rows, int64_t cols, int64_t gate_rows)
+// A run for each CU.  Teams that take whole groups by themselves add a gate's sums in their registers, but hold all its rows; if
+// all teams share a group's rows, its sums meet in LDS behind it, for about the time of two rows.  The fewer rows in turn: 5000 x
+// 512 with 16 rows to a gate take 41 us by groups and 23 by rows, 300 x 512 with 2 rows to a gate 13 and 39.
+static RunPlan plan_runs(int64_t rows, int64_t cols, int64_t gate_rows, bool gate)
 {
     const int64_t teams = cols <= 512 ? 16 : cols <= 1024 ? 8 : cols <= 2048 ? 4 : cols <= 4096 ? 2 : 1, most = 256;
+    auto run_of = [&](int64_t unit) { return ((rows + most - 1) / most + unit - 1) / unit * unit; };
     RunPlan p;
-    p.whole_groups = gate_rows <= 16;
-    const int64_t unit = teams * (p.whole_groups ? gate_rows : 1);
-    p.run = (int)(((rows + most - 1) / most + unit - 1) / unit * unit);
+    p.run = (int)run_of(teams);
+    p.whole_groups = false;
+    if (gate && gate_rows <= 16) {
+        const int64_t whole = run_of(teams * gate_rows);
+        p.whole_groups = whole / teams <= p.run / teams + 2 * ((p.run - 1) / gate_rows + 1);
+        if (p.whole_groups) p.run = (int)whole;
+    }
     p.runs = (int)((rows + p.run - 1) / p.run);
     return p;
 }
@@ -797,8 +812,13 @@ static void launch_grad(GradArgs a, hipStream_t stream)
     const int groups = (a.rows + a.gate_rows - 1) / a.gate_rows;
     const bool by_run = groups > a.runs;
     const int gates = a.dgate.p && !a.whole_groups ? std::min(groups, a.runs) : 0;
+    if (a.runs == 1 && row_fits(a.cols)) return;  // (the run's sums are the results)
+    // Sixteen gates to a workgroup where a gate has few runs: 2000 x 2048, 7 rows to a gate, 46 us with a workgroup for each, 27 so;
+    // 1920 x 136 with about nine runs to a gate 17 and 18.5.
+    const bool each_part = a.gate_rows <= 6 * a.run;
     if (a.dpre || a.dpost || gates)
-        residual_norm_sums_kernel<<<dim3((a.cols + 63) / 64, 2 + gates), 1024, 0, stream>>>(a, by_run);
+        residual_norm_sums_kernel<<<dim3((a.cols + 63) / 64, 2 + (each_part ? (gates + 15) / 16 : gates)), 1024, 0, stream>>>(
+            a, by_run, each_part, gates);
 }
 
 }  // namespace perf
@@ -851,7 +871,7 @@ extern "C" int64_t perf_residual_norm_backward_workspace_bytes(int64_t rows, int
     using namespace perf;
     if (rows < 1 || cols < 1 || rows > kMaxExtent8 || cols > kMaxExtent8) return -1;
     // (runs of whole groups are longer: there are no more of them)
-    const RunPlan p = plan_runs(rows, cols, INT64_MAX);
+    const RunPlan p = plan_runs(rows, cols, rows, false);
     return 4 * (4 * (int64_t)p.runs * cols + (row_fits(cols) ? 0 : rows));
 }
 
@@ -884,11 +904,11 @@ extern "C" perf_status perf_residual_norm_backward(const void *dy, const void *d
         return PERF_ERR_ALIGN;
     const int pb = param_dt == PERF_BF16, gb = gate_dt == PERF_BF16;
     const int per = (int)(gate ? std::min(gate_rows, rows) : rows);
-    const RunPlan p = plan_runs(rows, cols, per);
+    const RunPlan p = plan_runs(rows, cols, per, gate != nullptr);
     GradArgs a{dy ? dy : u, dh ? dh : u, dy ? h : u, u, dy != nullptr, dh != nullptr, Param{gate, gb}, Param{gamma_post, pb},
                Param{gamma_pre, pb}, rrms_post, rrms_pre, dx, du, Param{dgate, gb}, dgamma_post, dgamma_pre, (float *)workspace,
                dy ? lddy : ldu, dh ? lddh : ldu, dy ? ldh : ldu, ldu, ldg, lddx, lddu, lddg, (int)rows, (int)cols, per, div_magic(per),
-               p.run, p.runs, gate && p.whole_groups, residual_scale};
+               p.run, p.runs, p.whole_groups, residual_scale};
     if (x_dt == PERF_BF16)
         launch_grad<uint16_t>(a, (hipStream_t)stream);
     else

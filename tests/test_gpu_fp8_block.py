@@ -335,3 +335,13 @@ def test_gemm_choices_of_a_kernel(m, n, k):
     for c_dt in (F32, BF16):
         c = F.run_gemm(a, sa, b, sb, 128, c_dt)
         P.assert_contraction_close(c, ref, absdot, k + 3 + (2 ** 13 if c_dt == BF16 else 0), out_bf16=c_dt == BF16)
+
+
+@pytest.mark.parametrize("rows,cols,gate_rows", [(1, 700, 1), (6, 5760, 6), (12, 13128, 12), (16, 76, 16), (16, 76, 0), (145, 336, 13), (300, 512, 2),
+                                                 (2000, 2048, 7), (5000, 500, 16), (700, 300, 11), (1920, 136, 137), (400, 1000, 90)])
+@pytest.mark.parametrize("dt", [BF16, F32])
+def test_gradient_of_few_rows_and_of_small_groups(rows, cols, gate_rows, dt):
+    """One run of rows, whose sums are the results; groups taken by a team alone and by all; gates of two runs and of many."""
+    N._check_backward(rows, cols, dt, gate_rows)
+    N._check_backward(rows, cols, dt, gate_rows, F32, skip=("dpost",))
+    N._check_backward(rows, cols, dt, gate_rows, BF16, post=False, skip=("dgate", "dpre"))
