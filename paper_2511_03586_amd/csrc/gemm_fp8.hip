@@ -412,11 +412,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Ge
         if constexpr (B128) {
             const uint32_t bits = __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, next128));
             mantissa = __builtin_bit_cast(float, bits);
-            if constexpr (!WIDE) {
-                if (bits & 0x7f800000u) {  // (zero and subnormal numbers stay whole in the factor)
-                    exponent = (bits >> 23) & 0xff;
-                    mantissa = __builtin_bit_cast(float, (bits & 0x807fffffu) | 0x3f800000u);
-                }
+            if constexpr (!WIDE) {  // (within 2^60, so that no product of the instruction leaves fp32; the rest stays in the factor)
+                exponent = min(max((int)(bits >> 23 & 0xff), 127 - 60), 127 + 60);
+                mantissa = __builtin_ldexpf(mantissa, 127 - exponent);
             }
         }
         Fragment<WIDE> fragment_b[WIDE ? TN : 1];

@@ -252,3 +252,20 @@ def test_gemm_is_the_same_every_time():
         first = F.run_gemm(a, sa, b, sb, 1, F32)
         for _ in range(3):
             assert np.array_equal(first, F.run_gemm(a, sa, b, sb, 1, F32))
+
+
+@pytest.mark.parametrize("m,n,k", [(3, 200, 300), (200, 300, 256), (1930, 1921, 256), (3700, 3601, 300)])
+@pytest.mark.parametrize("ea,eb", [(-100, 110), (95, -120), (-126, 100), (60, -149)])
+@pytest.mark.parametrize("b_rows", [1, 128])
+def test_gemm_scales_at_the_ends_of_fp32(m, n, k, ea, eb, b_rows):
+    """One scale huge and one tiny (a subnormal one too): the results are ordinary numbers."""
+    g = np.random.default_rng(1)
+    a, _ = F.random_operand(g, m, k, 1)
+    b, _ = F.random_operand(g, n, k, 1)
+    sa = torch.full((m, F.up(k)), 2.0 ** ea)
+    sb = torch.full((F.up(n, b_rows), F.up(k)), 2.0 ** eb)
+    ref, absdot = F.gemm_ref(a, sa, b, sb, b_rows)
+    for c_dt in (F32, BF16):
+        c = F.run_gemm(a, sa, b, sb, b_rows, c_dt)
+        # scales of powers of two change no rounding as long as nothing leaves the normal numbers (2^-89 * 2^-9 at least does not)
+        P.assert_contraction_close(c, ref, absdot, k + 3 + (2 ** 13 if c_dt == BF16 else 0), out_bf16=c_dt == BF16)
