@@ -253,6 +253,7 @@ __global__ __launch_bounds__(64 * W) void gemm_fp8_waves_kernel(const Gemm8Args 
     }
 }
 
+constexpr int tile_stage_bytes(int BM, int BN) { return BM + BN <= 256 ? 256 * kBlock8 : 512 * kBlock8; }  // a power of two
 constexpr int kScaleStage = 2048;  // bytes of LDS for the scales of a block: one for each row of a tile of A and of B, or for 128 of B
 
 // WM x WN waves, each with TM x TN groups of 16 rows of A and of B.  LDS: two stages of a block of K, rows of 128 bytes whose
@@ -273,13 +274,14 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Ge
 {
     constexpr bool WIDE = sizeof(CT) == 4;
     constexpr int NW = WM * WN, BM = 16 * TM * WM, BN = 16 * TN * WN;
-    constexpr int kStage = (BM + BN) * kBlock8, kLoadsA = BM / (8 * NW), kLoadsB = BN / (8 * NW);
+    constexpr int kStage = tile_stage_bytes(BM, BN), kLoadsA = BM / (8 * NW), kLoadsB = BN / (8 * NW);
     // groups of A that are in registers or on their way there: four, or what the sums and B's scales leave room for
     constexpr int kAhead = TM == 8 && !B128 ? 2 : 4;
     constexpr int kScales = B128 ? BM + 64 : BM + BN;  // of a stage (in whole waves' fetches)
     static_assert(kScales * 4 <= kScaleStage && (2 * kStage) % (2 * kScaleStage) == 0 && (kStage & (kStage - 1)) == 0, "stages differ in one bit");
-    static_assert(kLoadsA == 4 && kLoadsB == 4 && kScales <= 64 * NW, "the loads divide among the waves");
-    static_assert((TM == 4 || TM == 8) && kBlock8 % (16 * TN) == 0, "the schedule of the loads; a wave's rows of B in one tile of scales");
+    static_assert(kLoadsA == 4 && kLoadsB == TN && kScales <= 64 * NW, "the loads divide among the waves");
+    static_assert(TM == 4 || TM == 8, "the schedule of the loads");
+    static_assert(TN == 4 || (TN == 3 && WIDE && !B128), "the order of the sums; a wave's rows of B in one tile of scales");
     // (one array of dynamic size: of several the compiler knows that a load into LDS and a read are of the same one, and waits
     // for every load in flight before each read, whatever their places in it)
     extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -315,13 +317,13 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Ge
     for (int i = 0; i < 4; ++i) {
         const int skip_a = i * NW * 8 * (int)g.lda, skip_b = i * NW * 8 * (int)g.ldb;
         from_a[i] = make_rsrc(tile_a + skip_a, max(bytes_a - skip_a, 0));
-        from_b[i] = make_rsrc(tile_b + skip_b, max(bytes_b - skip_b, 0));
+        if (i < kLoadsB) from_b[i] = make_rsrc(tile_b + skip_b, max(bytes_b - skip_b, 0));
     }
     auto load = [&](int kb, int i) {
         const uint32_t at = kb < blocks ? (uint32_t)kb * kBlock8 : kOutOfRange;
         char *to = smem + (kb & 1) * kStage + (i * NW + wave) * 1024;
         issue_load_to(from_a[i], off_a + at, 0, to);
-        issue_load_to(from_b[i], off_b + at, 0, to + BM * kBlock8);
+        if (i < kLoadsB) issue_load_to(from_b[i], off_b + at, 0, to + BM * kBlock8);
     };
     float next_scale;
     auto load_scale = [&](int kb) { next_scale = my_scale[min(kb, blocks - 1)]; };
@@ -355,7 +357,6 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Ge
         if constexpr (B128) next128 = *reinterpret_cast<const float *>(scales + (kb & 1) * kScaleStage + at_sb);
     };
 
-    static_assert(TN == 4, "the order of the sums");
     // p: the last four sums, not yet added (WIDE: a group's are begun together and added during the next)
     float4_t acc[TM][TN], p[WIDE ? 2 * TN : TN], fb[TN];
     float factor = 0.f;                   // of the group before
@@ -471,8 +472,10 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Ge
 #pragma unroll
                         for (int w = 0; w < 4; ++w) widen_two<A5>(next_a, a[(i + 1) % kAhead], q, w);
                     }
-                    add((i + TM - 1) % TM, q, factor);  // of the group before, or of the step before
-                    read_next(q);
+                    if (q < TN) {
+                        add((i + TM - 1) % TM, q, factor);  // of the group before, or of the step before
+                        read_next(q);
+                    }
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 if constexpr (i == 0) take_scales_b(kb);
@@ -508,9 +511,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Ge
     // registers, 8 or 16 bytes per lane in 16 rows, it took 10 to 17 thousand cycles of the 126 thousand of 4096 x 4096 x 4096.
     wait_vmem_and_lds<0>();
     wg_barrier();  // (everyone's loads into LDS have ended)
-    constexpr int kPer = 16 / (int)sizeof(CT), kChunks = 16 * TN / kPer, kRowsOut = 64 / kChunks;
-    static_assert(NW * 16 * TM * 16 * TN * (int)sizeof(CT) <= 2 * kStage, "the tile fits the stages");
-    char *const out = smem + wave * (16 * TM * 16 * TN * (int)sizeof(CT));
+    constexpr int kPer = 16 / (int)sizeof(CT), kChunks = 16 * 4 / kPer, kRowsOut = 64 / kChunks;  // (rows of TN = 3 as long as of 4)
+    static_assert(NW * 16 * TM * kChunks * 16 <= 2 * kStage, "the tile fits the stages");
+    char *const out = smem + wave * (16 * TM * kChunks * 16);
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         const int row = 16 * i + (lane & 15);
@@ -533,7 +536,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Ge
     for (int r = 0; r < 16 * TM; r += kRowsOut) {
         const int row_out = r + lane / kChunks, m = m0 + wm * 16 * TM + row_out;
         const uint4_t v = *reinterpret_cast<const uint4_t *>(out + (row_out * kChunks + (chunk ^ (row_out & (kChunks - 1)))) * 16);
-        if (m >= g.M || n >= g.N) continue;
+        if (m >= g.M || n >= g.N || (TN < 4 && chunk * kPer >= 16 * TN)) continue;
         CT *to = C + (int64_t)m * g.ldc + n;
         if (n + kPer <= g.N) {
             if constexpr (sizeof(CT) == 4)  // (past the caches, two whole lines: 16 x 2113 x 1152 x 264 68 -> 50 us; bf16's single ones: no gain)
@@ -578,10 +581,10 @@ static perf_status launch_tile(const Gemm8Args &g, hipStream_t stream)
         p.C = (CT *)g.C + b * g.strideC;
         const dim3 grid((unsigned)(tiles_m * tiles_n), (unsigned)std::min(kMaxGridYZ, g.batch - b));
         constexpr int BM = 16 * TM * WM, BN = 16 * TN * WN;
-        const int lds = 2 * (BM + BN) * kBlock8 + 2 * kScaleStage;
-        if (g.b_block_rows == kBlock8) {
-            if (!allow_lds<gemm_fp8_tile_kernel<TM, TN, WM, WN, true, A5, CT>>(lds)) return PERF_ERR_LAUNCH;
-            gemm_fp8_tile_kernel<TM, TN, WM, WN, true, A5, CT><<<grid, 64 * WM * WN, lds, stream>>>(p, (int)tiles_m, (int)tiles_n);
+        const int lds = 2 * tile_stage_bytes(BM, BN) + 2 * kScaleStage;
+        if (TN == 4 && g.b_block_rows == kBlock8) {
+            if (!allow_lds<gemm_fp8_tile_kernel<TM, 4, WM, WN, true, A5, CT>>(lds)) return PERF_ERR_LAUNCH;
+            gemm_fp8_tile_kernel<TM, 4, WM, WN, true, A5, CT><<<grid, 64 * WM * WN, lds, stream>>>(p, (int)tiles_m, (int)tiles_n);
         } else {
             if (!allow_lds<gemm_fp8_tile_kernel<TM, TN, WM, WN, false, A5, CT>>(lds)) return PERF_ERR_LAUNCH;
             gemm_fp8_tile_kernel<TM, TN, WM, WN, false, A5, CT><<<grid, 64 * WM * WN, lds, stream>>>(p, (int)tiles_m, (int)tiles_n);
@@ -647,6 +650,13 @@ static perf_status gemm8(const Gemm8Args &g, hipStream_t stream)
     // against 21; 128 of 64 rows, K = 2048 15.5 against 10.8, 256 of them 17.4 against 20.
     // (and a launch of the waves, whose tiles are smaller, does not hold 2^29 columns)
     const bool tiles = mid >= 200 ? g.M > 32 || blocks <= 8 || mid > (1 << 20) : mid >= 100 && g.M > 64 && blocks <= (WIDE ? 8 : 20);
+    // Tiles of 128 x 96, a quarter less work in a round of 256, where there are no more rounds of them: 1999 x 2999 x 5003 (384 or 512
+    // tiles) 92 and 78 us, 2176 x 2048 x 500 (272, 374) 13.6 and 11.6; with 256 and 352 tiles (K = 4096) 47 and 55.
+    if constexpr (WIDE) {
+        const int64_t narrow = ((g.M + 127) / 128) * ((g.N + 95) / 96) * g.batch;
+        if (tiles && g.b_block_rows == 1 && 4 * ((narrow + 255) / 256) < 5 * ((mid + 255) / 256))
+            return launch_tile<4, 3, 2, 2, A5, CT>(g, stream);
+    }
     if (tiles) return launch_tile<4, 4, 2, 2, A5, CT>(g, stream);
     if (g.M <= 16) return waves_by_columns<1, A5, CT>(g, stream);
     if (g.M <= 32) return waves_by_columns<2, A5, CT>(g, stream);

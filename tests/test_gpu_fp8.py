@@ -269,3 +269,10 @@ def test_gemm_scales_at_the_ends_of_fp32(m, n, k, ea, eb, b_rows):
         c = F.run_gemm(a, sa, b, sb, b_rows, c_dt)
         # scales of powers of two change no rounding as long as nothing leaves the normal numbers (2^-89 * 2^-9 at least does not)
         P.assert_contraction_close(c, ref, absdot, k + 3 + (2 ** 13 if c_dt == BF16 else 0), out_bf16=c_dt == BF16)
+
+
+@pytest.mark.parametrize("m,n,k", [(1999, 2999, 300), (2049, 2049, 129), (2050, 2113, 1000), (1153, 3650, 255)])
+def test_gemm_of_narrow_tiles(m, n, k):
+    """Numbers of tiles for which the product with a scale for each row of B takes narrower ones."""
+    _check_gemm(m, n, k, 1, F32, E5M2)
+    _check_gemm(m, n, k, 1, F32, alpha=0.5, ldc=n + 5)
