@@ -233,8 +233,8 @@ perf_status perf_eltwise(perf_eltwise_op op, const void *a, const void *b, void 
  * A linear layer Y = X W^T of X [tokens][in] and W [out][in] takes X by rows and W in tiles (row orientation), its input
  * gradient dY by rows and W transposed, its weight gradient dY and X transposed by blocks of 1.
  * A block with an infinity or a NaN reads back (s * q) as NaN where that element is, or everywhere.
- * Bytes between a row's end and its stride are left as they are.  ldq and ldqt of a multiple of 16 are what perf_gemm_fp8
- * takes.
+ * Results must not overlap x or each other.  Bytes between a row's end and its stride are left as they are.  ldq and ldqt of
+ * a multiple of 16 are what perf_gemm_fp8 takes.
  * Errors: NULL (x, both orientations, or half of one), SHAPE (dimension < 1 or > 2^30, ld too small, block_rows not 1 or
  * 128), DTYPE, ALIGN (x to its element, scales to 4 bytes), LAUNCH. */
 perf_status perf_quantize_fp8(const void *x, void *q, float *scales, void *qt, float *scales_t, int64_t rows, int64_t cols,
@@ -252,7 +252,7 @@ perf_status perf_quantize_fp8(const void *x, void *q, float *scales, void *qt, f
  *           stride ldsb; b_block_rows 1 (a scale for 128 elements of a row) or 128 (for a tile)
  *   C       device, M x N, row stride ldc, f32 or bf16
  *   batch   as in perf_gemm: matrix b starts stride* elements after matrix b-1 (strideSA and strideSB in scales)
- * The last block may be short; what lies in memory behind a row's K elements is not used.
+ * The last block may be short; what lies in memory behind a row's K elements is not used.  C must not overlap the operands.
  * Errors: NULL, SHAPE (dimension < 1 or > 2^30, ld too small, negative stride, batches overlapping in C, b_block_rows not 1
  * or 128, alpha not finite), DTYPE, ALIGN (A or B not 16-byte aligned, scales or C not aligned to their elements),
  * UNSUPPORTED (b_dt E5M2; lda, ldb, strideA or strideB not a multiple of 16; a row stride of A, B or their scales of 2^23 or
@@ -276,7 +276,7 @@ perf_status perf_gemm_fp8(const void *A, const float *scaleA, const void *B, con
  *             sample's (gate_rows = rows of a sample) or of each element's own (gate_rows = 1); or NULL
  *   gamma_post, gamma_pre   device, length cols, param_dt
  *   rrms_post, rrms_pre     device fp32[rows] or NULL: receive r1 and r2, which the gradient takes
- * h or y may be exactly u or x (same pointer, same stride, same type).
+ * h or y may be exactly u or x (same pointer, same stride, same type); nothing else may overlap.
  * Errors: NULL, SHAPE (rows/cols < 1 or > 2^30, ld too small, gate_rows < 1, eps < 0 or not finite, residual_scale not
  * finite), DTYPE, ALIGN (pointer not aligned to its element size), UNSUPPORTED (y_dt neither x_dt nor E4M3), LAUNCH. */
 perf_status perf_residual_norm(const void *u, const void *x, const void *gate, const void *gamma_post, const void *gamma_pre,
@@ -297,8 +297,8 @@ perf_status perf_residual_norm(const void *u, const void *x, const void *gate, c
  *   dgate                   as gate, row stride lddg; dgamma_post, dgamma_pre  device fp32[cols]; each may be NULL: not computed
  *   workspace               device, at least perf_residual_norm_backward_workspace_bytes(rows, cols) bytes, 4-byte aligned,
  *                           contents are scratch; calls that may run at the same time need one each
- * dx may be exactly dh and du exactly dy (same pointer, same stride).  The workspace's size is -1 for arguments that the
- * call would reject.
+ * dx may be exactly dh and du exactly dy (same pointer, same stride); nothing else may overlap.  The workspace's size is -1
+ * for arguments that the call would reject.
  * Errors: NULL (dy and dh, u, dx, du, workspace; h, gamma_pre or rrms_pre with dy; rrms_post with gamma_post; the gradient of
  * something not given), SHAPE, DTYPE, ALIGN as perf_residual_norm, LAUNCH. */
 int64_t perf_residual_norm_backward_workspace_bytes(int64_t rows, int64_t cols);

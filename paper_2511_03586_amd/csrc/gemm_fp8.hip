@@ -626,8 +626,11 @@ template <int TM, bool A5, typename CT>
 static perf_status waves_by_columns(const Gemm8Args &g, hipStream_t stream)
 {
     constexpr int64_t kEnough = 160;
-    const int64_t tiles_m = (g.M + 16 * TM - 1) / (16 * TM) * g.batch;
-    if (tiles_m * ((g.N + 63) / 64) >= kEnough) return launch_waves<TM, 4, A5, CT>(g, stream);
+    const int64_t tiles_m = (g.M + 16 * TM - 1) / (16 * TM) * g.batch, widest = tiles_m * ((g.N + 63) / 64);
+    // Of the widest, whose LDS takes a CU, no more than one round for few rows: of half the size there are two or three to a CU, and
+    // one loads while another adds its sums (1 x 65536 x 2048 32 -> 26.5 us, 1 x 32768 x 4096 31 -> 29; 160 tiles, 1 x 10240 x 8192:
+    // 14.3 with them and 16.3 with 320 of half the size).
+    if (widest >= kEnough && (TM > 2 || widest <= 256)) return launch_waves<TM, 4, A5, CT>(g, stream);
     if (tiles_m * ((g.N + 31) / 32) >= kEnough) return launch_waves<TM, 2, A5, CT>(g, stream);
     return launch_waves<TM, 1, A5, CT>(g, stream);
 }

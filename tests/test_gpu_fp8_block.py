@@ -345,3 +345,24 @@ def test_gradient_of_few_rows_and_of_small_groups(rows, cols, gate_rows, dt):
     N._check_backward(rows, cols, dt, gate_rows)
     N._check_backward(rows, cols, dt, gate_rows, F32, skip=("dpost",))
     N._check_backward(rows, cols, dt, gate_rows, BF16, post=False, skip=("dgate", "dpre"))
+
+
+def test_gemm_of_more_matrices_than_a_launch_holds():
+    """Batches beyond 65535, in both kernels' launches."""
+    g = np.random.default_rng(4)
+    for m, n, k, batch in ((1, 4, 20, 65539), (2, 3, 1100, 65537)):
+        a, sa = F.random_operand(g, m, k, 1)
+        b, sb = F.random_operand(g, n, k, 1)
+        ref, absdot = F.gemm_ref(a, sa, b, sb, 1)
+        ld, kb = F.up(k, 16) * 16, F.up(k)
+        ad, bd = torch.zeros((m, ld), dtype=torch.uint8, device="cuda"), torch.zeros((n, ld), dtype=torch.uint8, device="cuda")
+        ad[:, :k], bd[:, :k] = a.view(torch.uint8).cuda(), b.view(torch.uint8).cuda()
+        sad, sbd = sa.cuda(), sb.cuda()
+        scaled = torch.arange(1, batch + 1, device="cuda", dtype=torch.float32)[:, None, None] * sad  # each matrix its own scales
+        c = torch.zeros((batch, m, n), device="cuda")
+        perf.perf_gemm_fp8(ad.data_ptr(), scaled.data_ptr(), bd.data_ptr(), sbd.data_ptr(), c.data_ptr(), m, n, k, ld, kb, ld, kb, n, 1,
+                           batch, 0, m * kb, 0, 0, m * n, c_dt=F32, stream=G.stream())
+        torch.cuda.synchronize()
+        for i in (0, 1, 65534, 65535, 65536, batch - 1):
+            got = c[i].cpu().double().numpy()
+            assert np.all(np.abs(got - (i + 1) * ref) <= (k + 4) * 2.0 ** -23 * (i + 1) * absdot), (m, i)
