@@ -10,7 +10,7 @@
 // by 1.3e-5 of its norm, whatever K).  Below the rounding of a bf16 C, 1.6e-3, that does not show.  For an fp32 C the operands
 // are widened to bf16, exactly, and multiplied by v_mfma_f32_16x16x32_bf16, whose sums are fp32 (3e-8): half the rate.
 //
-//  * gemm_fp8_tile_kernel: operands pass through LDS, two stages of one block of K; a workgroup tile of 256 x 256 (bf16 C) or
+//  * gemm_fp8_tile_kernel: operands pass through LDS, two or four stages of one block of K; a workgroup tile of 256 x 256 (bf16 C) or
 //    128 x 128.  Bound by the matrix units at the clock that their power leaves (1.55 to 1.83 GHz) and by the additions
 //    beside them: 4096^3 bf16 C 65 us (2.1 PFLOP/s), fp32 C 122 us (1.1 PFLOP/s).
 //  * gemm_fp8_waves_kernel: few output tiles or few rows; the waves of a workgroup share one tile and divide the blocks
@@ -254,10 +254,12 @@ __global__ __launch_bounds__(64 * W) void gemm_fp8_waves_kernel(const Gemm8Args 
 }
 
 constexpr int tile_stage_bytes(int BM, int BN) { return BM + BN <= 256 ? 256 * kBlock8 : 512 * kBlock8; }  // a power of two
-constexpr int kScaleStage = 2048;  // bytes of LDS for the scales of a block: one for each row of a tile of A and of B, or for 128 of B
+constexpr int scale_stage_bytes(int waves) { return waves * 256; }  // the scales of a block: a lane's each
+// S stages of operands and twice as many of scales: those of a block are read when its operands are in registers already
+constexpr int tile_lds_bytes(int BM, int BN, int S, int waves) { return S * tile_stage_bytes(BM, BN) + 2 * S * scale_stage_bytes(waves); }
 
-// WM x WN waves, each with TM x TN groups of 16 rows of A and of B.  LDS: two stages of a block of K, rows of 128 bytes whose
-// 16-byte chunks are permuted as in mfma_tile.h (swz64), and the block's scales.
+// WM x WN waves, each with TM x TN groups of 16 rows of A and of B.  LDS: S stages of a block of K, rows of 128 bytes whose
+// 16-byte chunks are permuted as in mfma_tile.h (swz64), and the blocks' scales.
 //
 // A step multiplies a block: B's fragments stay in registers, A's pass by, up to four groups ahead; a sum is scaled and
 // added behind the third product after its own (a sum can be used some 50 cycles after its instruction; behind the fourth it
@@ -269,7 +271,7 @@ constexpr int kScaleStage = 2048;  // bytes of LDS for the scales of a block: on
 // The scale of a 128 x 128 tile of B (B128) is the same for all sums of a wave: its exponent goes into the matrix
 // instruction, its mantissa into the factor of A's scale, which leaves one multiply-add per sum, and no product of two
 // scales that could leave fp32's range.
-template <int TM, int TN, int WM, int WN, bool B128, bool A5, typename CT>
+template <int TM, int TN, int WM, int WN, int S, bool B128, bool A5, typename CT>
 __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Gemm8Args g, int tiles_m, int tiles_n)
 {
     constexpr bool WIDE = sizeof(CT) == 4;
@@ -277,15 +279,16 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Ge
     constexpr int kStage = tile_stage_bytes(BM, BN), kLoadsA = BM / (8 * NW), kLoadsB = BN / (8 * NW);
     // groups of A that are in registers or on their way there: four, or what the sums and B's scales leave room for
     constexpr int kAhead = TM == 8 && !B128 ? 2 : 4;
-    constexpr int kScales = B128 ? BM + 64 : BM + BN;  // of a stage (in whole waves' fetches)
-    static_assert(kScales * 4 <= kScaleStage && (2 * kStage) % (2 * kScaleStage) == 0 && (kStage & (kStage - 1)) == 0, "stages differ in one bit");
-    static_assert(kLoadsA == 4 && kLoadsB == TN && kScales <= 64 * NW, "the loads divide among the waves");
+    constexpr int kScaleStage = scale_stage_bytes(NW), kScalesAt = 0, kTilesAt = 2 * S * kScaleStage;
+    constexpr int kInFlight = kLoadsA + kLoadsB + 1;  // loads of a block
+    static_assert((S & (S - 1)) == 0 && (kStage & (kStage - 1)) == 0 && (kScaleStage & (kScaleStage - 1)) == 0, "places wrap by a mask");
+    static_assert(kLoadsA == 4 && kLoadsB == TN && (B128 ? BM + 64 : BM + BN) <= 64 * NW, "the loads divide among the waves");
     static_assert(TM == 4 || TM == 8, "the schedule of the loads");
     static_assert(TN == 4 || (TN == 3 && WIDE && !B128), "the order of the sums; a wave's rows of B in one tile of scales");
     // (one array of dynamic size: of several the compiler knows that a load into LDS and a read are of the same one, and waits
     // for every load in flight before each read, whatever their places in it)
     extern __shared__ __attribute__((aligned(1024))) char smem[];
-    char *const scales = smem + 2 * kStage;  // two stages of kScaleStage bytes
+    char *const scales = smem + kScalesAt, *const tiles = smem + kTilesAt;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const int64_t bz = blockIdx.y;
@@ -302,13 +305,17 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Ge
     const uint32_t off_a = (uint32_t)(row * g.lda) + chunk_at, off_b = (uint32_t)(row * g.ldb) + chunk_at;
     static_assert(NW * 8 % 16 == 0, "the permutation repeats after 16 rows");
     // the row of scales that this lane fetches for all: A's, then B's, of which a tile of B128 has one for 128 rows
-    const int slot = wave * 64 + lane;
-    const bool fetches = wave * 64 < kScales;
-    const float *my_scale = g.sa + bz * g.strideSA + (int64_t)(m0 + min(slot, rows_m - 1)) * g.ldsa;
-    if (slot >= BM) {
-        const int n = B128 ? min(n0 / kBlock8 + slot - BM, (g.N - 1) / kBlock8) : n0 + min(slot - BM, rows_n - 1);
-        my_scale = g.sb + bz * g.strideSB + (int64_t)n * g.ldsb;
-    }
+    const int slot = wave * 64;
+    const bool of_a = slot < BM;
+    auto scale_row = [&](int slot) {
+        if (of_a) return m0 + min(slot, rows_m - 1);
+        return B128 ? min(n0 / kBlock8 + slot - BM, (g.N - 1) / kBlock8) : n0 + min(slot - BM, rows_n - 1);
+    };
+    const int first_scale = scale_row(slot);
+    const int64_t ld_scales = of_a ? g.ldsa : g.ldsb;
+    const rsrc_t from_scales = make_rsrc((of_a ? g.sa + bz * g.strideSA : g.sb + bz * g.strideSB) + first_scale * ld_scales,
+                                         (uint32_t)(((scale_row(slot + 63) - first_scale) * ld_scales + blocks) * 4));
+    const uint32_t off_scale = (uint32_t)((scale_row(slot + lane) - first_scale) * ld_scales * 4);
     // Load i of a block begins with row 8 NW i and ends with the operand: what is behind (rows past the matrix among it) reads
     // as zero.  A load of a block past the last one is out of range altogether: it moves nothing, and the number in flight is
     // the same.
@@ -321,40 +328,43 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Ge
     }
     auto load = [&](int kb, int i) {
         const uint32_t at = kb < blocks ? (uint32_t)kb * kBlock8 : kOutOfRange;
-        char *to = smem + (kb & 1) * kStage + (i * NW + wave) * 1024;
+        char *to = tiles + (kb & (S - 1)) * kStage + (i * NW + wave) * 1024;
         issue_load_to(from_a[i], off_a + at, 0, to);
         if (i < kLoadsB) issue_load_to(from_b[i], off_b + at, 0, to + BM * kBlock8);
     };
-    float next_scale;
-    auto load_scale = [&](int kb) { next_scale = my_scale[min(kb, blocks - 1)]; };
-    auto put_scale = [&](int kb) {
-        if (fetches) *reinterpret_cast<float *>(scales + (kb & 1) * kScaleStage + slot * 4) = next_scale;
+    auto load_scale = [&](int kb) {
+        const uint32_t at = kb < blocks ? (uint32_t)kb * 4 : kOutOfRange;
+        char *to = scales + (kb & (2 * S - 1)) * kScaleStage + wave * 256;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from_scales, (__attribute__((address_space(3))) void *)to, 4, off_scale + at, 0, 0, 0);
     };
 
     // This lane's places in a stage: of its half fragments of A and B (rows are 16 apart from group to group, which leaves the
-    // permutation as it is) and of the scales of its row of A and its four of B.  They change stages by one bit.
+    // permutation as it is) and of the scales of its row of A and its four of B.
     const int row_a = wm * 16 * TM, row_b = BM + wn * 16 * TN;
-    int at_a[2], at_b[2], at_sa = 2 * kStage + (row_a + (lane & 15)) * 4;
+    int at_a[2], at_b[2], at_sa = (row_a + (lane & 15)) * 4;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         at_a[h] = row_a * kBlock8 + frag_offset64(lane & 15, (lane >> 4) + 4 * h);
         at_b[h] = row_b * kBlock8 + frag_offset64(lane & 15, (lane >> 4) + 4 * h);
     }
     const int at_sb = B128 ? (BM + wn * 16 * TN / kBlock8) * 4 : (row_b + 4 * (lane >> 4)) * 4;  // from the stage's scales on
-    auto other_stage = [&](int (&at)[2]) { at[0] ^= kStage, at[1] ^= kStage; };
+    auto next_stage = [&](int (&at)[2]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) at[h] = S == 2 ? at[h] ^ kStage : (at[h] + kStage) & (S * kStage - 1);
+    };
     auto read = [&](const int (&at)[2], int row) {
-        const int4v_t lo = *reinterpret_cast<const int4v_t *>(smem + at[0] + row * kBlock8);
-        const int4v_t hi = *reinterpret_cast<const int4v_t *>(smem + at[1] + row * kBlock8);
+        const int4v_t lo = *reinterpret_cast<const int4v_t *>(tiles + at[0] + row * kBlock8);
+        const int4v_t hi = *reinterpret_cast<const int4v_t *>(tiles + at[1] + row * kBlock8);
         return int8v_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     };
     int8v_t a[kAhead], b[TN];
     float fa[kAhead], next128 = 1.f;
     auto read_a = [&](int i) {
         a[i % kAhead] = read(at_a, 16 * i);
-        fa[i % kAhead] = *reinterpret_cast<const float *>(smem + at_sa + 64 * i);
+        fa[i % kAhead] = *reinterpret_cast<const float *>(scales + at_sa + 64 * i);
     };
     auto read_128 = [&](int kb) {
-        if constexpr (B128) next128 = *reinterpret_cast<const float *>(scales + (kb & 1) * kScaleStage + at_sb);
+        if constexpr (B128) next128 = *reinterpret_cast<const float *>(scales + (kb & (2 * S - 1)) * kScaleStage + at_sb);
     };
 
     // p: the last four sums, not yet added (WIDE: a group's are begun together and added during the next)
@@ -381,17 +391,15 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Ge
         asm volatile("" : "+v"(acc[i][j]));
     };
 
-    // the first two blocks; the first is waited for
-    load_scale(0);
+    // the first S blocks; the first is waited for
 #pragma unroll
-    for (int i = 0; i < 4; ++i) load(0, i);
-    wait_vmem<0>();
-    put_scale(0);
-    wait_vmem_and_lds<0>();
+    for (int kb = 0; kb < S; ++kb) {
+        load_scale(kb);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load(kb, i);
+    }
+    wait_vmem<(S - 1) * kInFlight>();
     wg_barrier();
-    load_scale(1);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) load(1, i);
 #pragma unroll
     for (int j = 0; j < TN; ++j) b[j] = read(at_b, 16 * j);
 #pragma unroll
@@ -401,7 +409,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Ge
     auto take_scales_b = [&](int kb) {
         if constexpr (!B128) {
 #pragma unroll
-            for (int j = 0; j < TN; ++j) fb[j] = *reinterpret_cast<const float4_t *>(scales + (kb & 1) * kScaleStage + at_sb + 64 * j);
+            for (int j = 0; j < TN; ++j) fb[j] = *reinterpret_cast<const float4_t *>(scales + (kb & (2 * S - 1)) * kScaleStage + at_sb + 64 * j);
         }
     };
     Fragment<WIDE> next_a;  // (WIDE) the next group's fragment, widened during this one's products
@@ -432,24 +440,23 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Ge
         unrolled<TM>([&](auto group) {
             constexpr int i = decltype(group)::value;
             if constexpr (i == TM - kAhead) {
-                wait_vmem<0>();
-                put_scale(kb + 1);
+                wait_vmem<(S - 2) * kInFlight>();
                 wait_lds();
                 wg_barrier();
-                load_scale(kb + 2);
+                load_scale(kb + S);
             }
             if constexpr (i >= TM - kAhead) {
 #pragma unroll
-                for (int l = 0; l < 4 / kAhead; ++l) load(kb + 2, (i - (TM - kAhead)) * (4 / kAhead) + l);
+                for (int l = 0; l < 4 / kAhead; ++l) load(kb + S, (i - (TM - kAhead)) * (4 / kAhead) + l);
             }
             const float f = fa[i % kAhead] * mantissa;
             auto read_next = [&](int j) {  // into the places of what has been used for the last time
                 if constexpr (i == TM - 1) {
-                    if (j == 0) other_stage(at_b);
+                    if (j == 0) next_stage(at_b);
                     b[j] = read(at_b, 16 * j);
                 }
                 if (j == TN - 1) {
-                    if constexpr (i == TM - kAhead) other_stage(at_a), at_sa ^= kScaleStage;
+                    if constexpr (i == TM - kAhead) next_stage(at_a), at_sa = (at_sa + kScaleStage) & (2 * S * kScaleStage - 1);
                     read_a((i + kAhead) % TM);
                     if constexpr (i == TM - 1) read_128(kb + 1);
                 }
@@ -512,8 +519,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Ge
     wait_vmem_and_lds<0>();
     wg_barrier();  // (everyone's loads into LDS have ended)
     constexpr int kPer = 16 / (int)sizeof(CT), kChunks = 16 * 4 / kPer, kRowsOut = 64 / kChunks;  // (rows of TN = 3 as long as of 4)
-    static_assert(NW * 16 * TM * kChunks * 16 <= 2 * kStage, "the tile fits the stages");
-    char *const out = smem + wave * (16 * TM * kChunks * 16);
+    static_assert(NW * 16 * TM * kChunks * 16 <= S * kStage, "the tile fits the stages");
+    char *const out = tiles + wave * (16 * TM * kChunks * 16);
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         const int row = 16 * i + (lane & 15);
@@ -570,7 +577,7 @@ static bool allow_lds(int bytes)
     return true;
 }
 
-template <int TM, int TN, int WM, int WN, bool A5, typename CT>
+template <int TM, int TN, int WM, int WN, int S, bool A5, typename CT>
 static perf_status launch_tile(const Gemm8Args &g, hipStream_t stream)
 {
     const int64_t tiles_m = (g.M + 16 * TM * WM - 1) / (16 * TM * WM), tiles_n = (g.N + 16 * TN * WN - 1) / (16 * TN * WN);
@@ -581,13 +588,13 @@ static perf_status launch_tile(const Gemm8Args &g, hipStream_t stream)
         p.C = (CT *)g.C + b * g.strideC;
         const dim3 grid((unsigned)(tiles_m * tiles_n), (unsigned)std::min(kMaxGridYZ, g.batch - b));
         constexpr int BM = 16 * TM * WM, BN = 16 * TN * WN;
-        const int lds = 2 * tile_stage_bytes(BM, BN) + 2 * kScaleStage;
+        constexpr int lds = tile_lds_bytes(BM, BN, S, WM * WN);
         if (TN == 4 && g.b_block_rows == kBlock8) {
-            if (!allow_lds<gemm_fp8_tile_kernel<TM, 4, WM, WN, true, A5, CT>>(lds)) return PERF_ERR_LAUNCH;
-            gemm_fp8_tile_kernel<TM, 4, WM, WN, true, A5, CT><<<grid, 64 * WM * WN, lds, stream>>>(p, (int)tiles_m, (int)tiles_n);
+            if (!allow_lds<gemm_fp8_tile_kernel<TM, 4, WM, WN, S, true, A5, CT>>(lds)) return PERF_ERR_LAUNCH;
+            gemm_fp8_tile_kernel<TM, 4, WM, WN, S, true, A5, CT><<<grid, 64 * WM * WN, lds, stream>>>(p, (int)tiles_m, (int)tiles_n);
         } else {
-            if (!allow_lds<gemm_fp8_tile_kernel<TM, TN, WM, WN, false, A5, CT>>(lds)) return PERF_ERR_LAUNCH;
-            gemm_fp8_tile_kernel<TM, TN, WM, WN, false, A5, CT><<<grid, 64 * WM * WN, lds, stream>>>(p, (int)tiles_m, (int)tiles_n);
+            if (!allow_lds<gemm_fp8_tile_kernel<TM, TN, WM, WN, S, false, A5, CT>>(lds)) return PERF_ERR_LAUNCH;
+            gemm_fp8_tile_kernel<TM, TN, WM, WN, S, false, A5, CT><<<grid, 64 * WM * WN, lds, stream>>>(p, (int)tiles_m, (int)tiles_n);
         }
         const perf_status st = launch_status();
         if (st != PERF_OK) return st;
@@ -644,23 +651,27 @@ static perf_status gemm8(const Gemm8Args &g, hipStream_t stream)
     // A round of 256 tiles of 256 x 256 takes as long as 2.4 of 128 x 128 (K = 4096, N = 4096: 50 us; 41 for two of the latter, 63
     // for three), so the larger ones pay from three rounds of the smaller on.
     if constexpr (!WIDE) {
-        if (12 * ((big + 255) / 256) < 5 * ((mid + 255) / 256)) return launch_tile<8, 4, 2, 4, A5, CT>(g, stream);
+        if (12 * ((big + 255) / 256) < 5 * ((mid + 255) / 256)) return launch_tile<8, 4, 2, 4, 2, A5, CT>(g, stream);
     }
-    // A tile kernel on less than the whole chip begins sooner, the waves that divide K then go on faster.  128 tiles: K = 1024
-    // 8.8 us against 12.7, K = 4096 26.7 against 23.3 (bf16 C); K = 700 13.0 against 14.1, K = 4096 42 against 29.5 (fp32 C).
-    // 256 tiles, K = 4096: 28.5 against 36 (bf16), 45 against 54 (fp32).  64 tiles, K = 8192: 47 against 20.
-    // Few rows leave a tile part empty: 256 tiles of 32 rows, K = 4096 41 against 33 (fp32 50 against 33), 512 of them, K = 1024 15.4
-    // against 21; 128 of 64 rows, K = 2048 15.5 against 10.8, 256 of them 17.4 against 20.
+    // A tile takes its time however few there are, the waves that divide K theirs for each.  192 tiles, K = 3000: 19.5 us against
+    // 30.7 (bf16 C); 128 tiles: K = 1024 8.6 against 12.7, K = 4096 21.3 against 23.2, K = 14336 66 against 60; fp32 C: 256 tiles,
+    // K = 4096 38 against 54, 128 tiles, K = 700 13.0 against 14.1, K = 4096 37 against 27.  64 tiles, K = 8192: 36 against 20.
+    // Few rows leave a tile part empty: 256 tiles of 32 rows, K = 4096 36 against 33 (fp32 50 against 33), 512 of them, K = 1024 15.4
+    // against 21; 128 of 64 rows, K = 4096 21 against 15.4, 256 of them, K = 2048 17.4 against 20.
     // (and a launch of the waves, whose tiles are smaller, does not hold 2^29 columns)
-    const bool tiles = mid >= 200 ? g.M > 32 || blocks <= 8 || mid > (1 << 20) : mid >= 100 && g.M > 64 && blocks <= (WIDE ? 8 : 20);
+    const bool tiles = mid >= 200 ? g.M > 32 || blocks <= 8 || mid > (1 << 20)
+                                  : g.M > 64 && (mid >= (WIDE ? 176 : 140) || (mid >= 100 && blocks <= (WIDE ? 8 : 32)));
     // Tiles of 128 x 96, a quarter less work in a round of 256, where there are no more rounds of them: 1999 x 2999 x 5003 (384 or 512
     // tiles) 92 and 78 us, 2176 x 2048 x 500 (272, 374) 13.6 and 11.6; with 256 and 352 tiles (K = 4096) 47 and 55.
     if constexpr (WIDE) {
         const int64_t narrow = ((g.M + 127) / 128) * ((g.N + 95) / 96) * g.batch;
         if (tiles && g.b_block_rows == 1 && 4 * ((narrow + 255) / 256) < 5 * ((mid + 255) / 256))
-            return launch_tile<4, 3, 2, 2, A5, CT>(g, stream);
+            return launch_tile<4, 3, 2, 2, 2, A5, CT>(g, stream);
     }
-    if (tiles) return launch_tile<4, 4, 2, 2, A5, CT>(g, stream);
+    // One workgroup to a CU, so that its stages can be four: 1024 x 4096 x 4096 27.7 -> 24 us.  (Of two to a CU one hides the other's
+    // loads: 2048 x 4096 x 4096 41.5 us with two stages each, 47 with four.)
+    if (tiles && mid <= 256) return launch_tile<4, 4, 2, 2, 4, A5, CT>(g, stream);
+    if (tiles) return launch_tile<4, 4, 2, 2, 2, A5, CT>(g, stream);
     if (g.M <= 16) return waves_by_columns<1, A5, CT>(g, stream);
     if (g.M <= 32) return waves_by_columns<2, A5, CT>(g, stream);
     return waves_by_columns<4, A5, CT>(g, stream);

@@ -276,3 +276,11 @@ def test_gemm_of_narrow_tiles(m, n, k):
     """Numbers of tiles for which the product with a scale for each row of B takes narrower ones."""
     _check_gemm(m, n, k, 1, F32, E5M2)
     _check_gemm(m, n, k, 1, F32, alpha=0.5, ldc=n + 5)
+
+
+@pytest.mark.parametrize("m,n,k", [(700, 3500, 128), (1025, 2000, 130), (1500, 1700, 513), (130, 16300, 700), (1100, 2100, 2900), (2048, 2048, 640)])
+@pytest.mark.parametrize("b_rows", [1, 128])
+def test_gemm_of_one_round_of_tiles(m, n, k, b_rows):
+    """From 100 to 256 tiles, K from one block to more than the stages hold."""
+    _check_gemm(m, n, k, b_rows, BF16, ldsa=F.up(k) + 3, ldsb=F.up(k) + 1)
+    _check_gemm(m, n, k, b_rows, F32, E5M2)
