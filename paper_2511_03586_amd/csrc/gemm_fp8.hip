@@ -658,9 +658,13 @@ static perf_status gemm8(const Gemm8Args &g, hipStream_t stream)
     // K = 4096 38 against 54, 128 tiles, K = 700 13.0 against 14.1, K = 4096 37 against 27.  64 tiles, K = 8192: 36 against 20.
     // Few rows leave a tile part empty: 256 tiles of 32 rows, K = 4096 36 against 33 (fp32 50 against 33), 512 of them, K = 1024 15.4
     // against 21; 128 of 64 rows, K = 4096 21 against 15.4, 256 of them, K = 2048 17.4 against 20.
+    // The waves' 64 x 64 tiles take a CU each: beyond 256 of them a second round begins.  700 x 1500 x 300 8.5 us in tiles against 11
+    // (both C), 2700 x 400 x 713 9.1 against 12.8, 1024 x 1536 x 2048 15.4 against 16.8 (bf16), 18.5 in both (fp32).
     // (and a launch of the waves, whose tiles are smaller, does not hold 2^29 columns)
+    const int64_t waves = ((g.M + 63) / 64) * ((g.N + 63) / 64) * g.batch;
     const bool tiles = mid >= 200 ? g.M > 32 || blocks <= 8 || mid > (1 << 20)
-                                  : g.M > 64 && (mid >= (WIDE ? 176 : 140) || (mid >= 100 && blocks <= (WIDE ? 8 : 32)));
+                                  : g.M > 64 && (mid >= (WIDE ? 176 : 140) || (mid >= 100 && blocks <= (WIDE ? 8 : 32)) ||
+                                                 (waves > 256 && blocks <= (WIDE ? 8 : 16)));
     // Tiles of 128 x 96, a quarter less work in a round of 256, where there are no more rounds of them: 1999 x 2999 x 5003 (384 or 512
     // tiles) 92 and 78 us, 2176 x 2048 x 500 (272, 374) 13.6 and 11.6; with 256 and 352 tiles (K = 4096) 47 and 55.
     if constexpr (WIDE) {

@@ -284,3 +284,9 @@ def test_gemm_of_one_round_of_tiles(m, n, k, b_rows):
     """From 100 to 256 tiles, K from one block to more than the stages hold."""
     _check_gemm(m, n, k, b_rows, BF16, ldsa=F.up(k) + 3, ldsb=F.up(k) + 1)
     _check_gemm(m, n, k, b_rows, F32, E5M2)
+
+
+@pytest.mark.parametrize("m,n,k", [(700, 1500, 300), (2700, 400, 713), (1024, 1536, 2100), (65, 17000, 256), (70, 16300, 1200)])
+def test_gemm_of_more_than_one_round_of_small_tiles(m, n, k):
+    _check_gemm(m, n, k, 128, BF16)
+    _check_gemm(m, n, k, 1, F32, E5M2)
