@@ -66,7 +66,6 @@ __device__ __forceinline__ uint32_t group_max_u32(uint32_t v)
 template <typename T> struct Eight;
 template <> struct Eight<uint16_t> {
     uint4_t raw;
-    __device__ __forceinline__ void clear() { raw = uint4_t{0, 0, 0, 0}; }
     // makes the compiler take the elements for new ones: it then unpacks them again and does not keep what it unpacked before
     __device__ __forceinline__ void renew()
     {
@@ -116,7 +115,6 @@ template <> struct Eight<uint16_t> {
 };
 template <> struct Eight<float> {
     uint4_t lo, hi;
-    __device__ __forceinline__ void clear() { lo = hi = uint4_t{0, 0, 0, 0}; }
     __device__ __forceinline__ void renew()
     {
 #pragma unroll

@@ -29,7 +29,6 @@ template <typename T> struct Sixteen {
         h[0].load(p, n);
         h[1].load(p + 8, n - 8);
     }
-    __device__ __forceinline__ void clear() { h[0].clear(), h[1].clear(); }
     __device__ __forceinline__ void get(float (&v)[16]) const
     {
         float a[8], b[8];
