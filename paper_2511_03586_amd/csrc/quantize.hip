@@ -298,8 +298,8 @@ template <typename T, bool E5M2>
 static perf_status launch_rows(const QuantizeArgs &a)
 {
     const int64_t blocks = (a.cols + kBlock8 - 1) / kBlock8;
-    // a launch covers fewer than 2^31 blocks, and no more than 2^32 threads
-    const int64_t most = (int64_t)((1ll << 29) - 1) / blocks;
+    // rows of a launch, which is less than 2^32 threads: a workgroup quantises 32 blocks
+    const int64_t most = max_blocks(256) * 32 / blocks;
     for (int64_t r = 0; r < a.rows; r += most) {
         const int64_t rows = std::min(most, a.rows - r), items = rows * blocks * 8;
         quantize_rows_kernel<T, E5M2><<<(unsigned)((items + 255) / 256), 256, 0, a.stream>>>(

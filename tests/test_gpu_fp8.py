@@ -109,6 +109,22 @@ def test_quantize_large_offsets():
     assert torch.equal(st.get(), rs)
 
 
+def test_quantize_of_more_blocks_than_a_launch_holds():
+    """Rows of one block each, more than 2^29 of them (a dimension of 2^32 threads is cut short without an error): every element
+    and scale is that of its value, of which there are seven."""
+    rows, piece = (1 << 29) + 1000, 7 << 23
+    few = torch.tensor([[0.0], [1.5], [-3.0], [0.3125], [1e-3], [-700.0], [5e30]]).to(torch.bfloat16)
+    rq, rs = F.quantize_ref(few, 1, E4M3)
+    few, rq, rs = few[:, 0].cuda(), rq.view(torch.uint8)[:, 0].cuda(), rs[:, 0].cuda()
+    x = few.repeat(F.up(rows, 7))[:rows]
+    q = torch.full((rows,), F.GUARD, dtype=torch.uint8, device="cuda")
+    s = torch.full((rows,), float("nan"), device="cuda")
+    perf.perf_quantize_fp8(x.data_ptr(), q.data_ptr(), s.data_ptr(), None, None, rows, 1, 1, 1, 1, 0, 0, 1, BF16, E4M3, stream=G.stream())
+    for i in range(0, rows, piece):
+        n = min(piece, rows - i)
+        assert torch.equal(q[i:i + n], rq.repeat(F.up(n, 7))[:n]) and torch.equal(s[i:i + n], rs.repeat(F.up(n, 7))[:n]), i
+
+
 # ---- product ----------------------------------------------------------------------------------------
 def _check_gemm(m, n, k, b_rows, c_dt, a_dt=E4M3, alpha=1.0, seed=0, **kw):
     g = np.random.default_rng(1000 * m + 10 * n + k + seed)
