@@ -586,14 +586,15 @@ __global__ __launch_bounds__(1024) void residual_norm_grad_kernel(const GradArgs
     }
 }
 
-// The runs' sums, added in the order of the rows, 64 columns per workgroup.  blockIdx.y: 0 = dgamma_pre, 1 = dgamma_post, sixteen
-// parts of the runs side by side; then the gates of groups that begin in one run and go on beyond it, by group or (by_run) by
-// the run in which it begins, whichever are fewer: one gate in sixteen parts, or sixteen gates (each_part) of few runs.
-__global__ __launch_bounds__(1024) void residual_norm_sums_kernel(const GradArgs a, bool by_run, bool each_part, int gates)
+// The runs' sums, added in the order of the rows, 64 columns per workgroup, from column `first` on.  blockIdx.y: 0 = dgamma_pre,
+// 1 = dgamma_post, sixteen parts of the runs side by side; then the gates of groups that begin in one run and go on beyond it, by
+// group or (by_run) by the run in which it begins, whichever are fewer: one gate in sixteen parts, or sixteen gates (each_part) of
+// few runs.
+__global__ __launch_bounds__(1024) void residual_norm_sums_kernel(const GradArgs a, bool by_run, bool each_part, int gates, int first)
 {
     constexpr int kParts = 16;
     __shared__ float parts[kParts][64];
-    const int lane = threadIdx.x & 63, part = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = blockIdx.x * 64 + lane;
+    const int lane = threadIdx.x & 63, part = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = first + blockIdx.x * 64 + lane;
     const bool gamma = blockIdx.y < 2, post = blockIdx.y == 1;
     const int gate = each_part ? (blockIdx.y - 2) * kParts + part : blockIdx.y - 2;
     int count = a.runs, g = 0;
@@ -816,9 +817,11 @@ static void launch_grad(GradArgs a, hipStream_t stream)
     // Sixteen gates to a workgroup where a gate has few runs: 2000 x 2048, 7 rows to a gate, 46 us with a workgroup for each, 27 so;
     // 1920 x 136 with about nine runs to a gate 17 and 18.5.
     const bool each_part = a.gate_rows <= 6 * a.run;
-    if (a.dpre || a.dpost || gates)
-        residual_norm_sums_kernel<<<dim3((a.cols + 63) / 64, 2 + (each_part ? (gates + 15) / 16 : gates)), 1024, 0, stream>>>(
-            a, by_run, each_part, gates);
+    if (!a.dpre && !a.dpost && !gates) return;
+    constexpr int kMost = (int)max_blocks(1024) * 64;  // columns of a launch, which is less than 2^32 threads
+    for (int64_t first = 0; first < a.cols; first += kMost)
+        residual_norm_sums_kernel<<<dim3(((int)std::min<int64_t>(kMost, a.cols - first) + 63) / 64, 2 + (each_part ? (gates + 15) / 16 : gates)),
+                                    1024, 0, stream>>>(a, by_run, each_part, gates, (int)first);
 }
 
 }  // namespace perf

@@ -54,3 +54,43 @@ def test_quantize_rows_are_all_launched(recorder):
             assert items % (8 * up(cols)) == 0 and l["grid"][0] * l["block"][0] >= items > 0
             done += items // (8 * up(cols))
         assert done == rows, (rows, cols)
+
+
+def _norm(rows, cols, gate_rows, x_dt, y_dt):
+    return ("perf_residual_norm", dict(u=FAKE, x=FAKE, gate=FAKE if gate_rows else None, gamma_post=FAKE, gamma_pre=FAKE, h=FAKE, y=FAKE,
+                                       y_scales=FAKE, rrms_post=FAKE, rrms_pre=FAKE, rows=rows, cols=cols, ldu=cols, ldx=cols, ldg=cols,
+                                       gate_rows=gate_rows, ldh=cols, ldy=cols, lds=up(cols), residual_scale=1.0, eps=1e-5, x_dt=x_dt,
+                                       y_dt=y_dt))
+
+
+def _norm_gradient(rows, cols, gate_rows, x_dt):
+    gate = FAKE if gate_rows else None
+    return ("perf_residual_norm_backward", dict(dy=FAKE, dh=FAKE, h=FAKE, u=FAKE, gate=gate, gamma_post=FAKE, gamma_pre=FAKE, rrms_post=FAKE,
+                                                rrms_pre=FAKE, dx=FAKE, du=FAKE, dgate=gate, dgamma_post=FAKE, dgamma_pre=FAKE,
+                                                workspace=FAKE, rows=rows, cols=cols, lddy=cols, lddh=cols, ldh=cols, ldu=cols, ldg=cols,
+                                                gate_rows=gate_rows, lddx=cols, lddu=cols, lddg=cols, residual_scale=1.0, x_dt=x_dt))
+
+
+# rows of every number of waves, and those that are not held in registers, to the ends
+NORMS = [(rows, cols) for cols in (1, 7, 8, 512, 513, 4096, 16384, 16385, 1 << 20, (1 << 28) - 64, (1 << 28) - 63, 1 << 28, MOST)
+         for rows in (1, 2, 255, 256, 257, 4097, 1 << 20, MOST) if rows * cols <= 1 << 37]
+
+
+def test_norm_grids(recorder):
+    _check_grids(L.record(recorder, [_norm(r, c, g, dt, y) for r, c in NORMS for g in (0, 1, 16, 1000, r)
+                                     for dt, y in ((BF16, E4M3), (F32, F32))]))
+
+
+def test_norm_gradient_grids(recorder):
+    _check_grids(L.record(recorder, [_norm_gradient(r, c, g, dt) for r, c in NORMS for g in (0, 1, 16, 1000, r) for dt in (BF16, F32)]))
+
+
+def test_norm_gradient_sums_of_all_columns_are_launched(recorder):
+    """64 columns to a workgroup; a launch takes up where the one before it ends."""
+    for (rows, cols), r in zip(NORMS, L.record(recorder, [_norm_gradient(r, c, 0, BF16) for r, c in NORMS], "residual_norm_sums_kernel", 5)):
+        done = 0
+        for l in r["launches"]:
+            if "residual_norm_sums_kernel" in l["name"]:
+                assert ctypes.c_int32(l["args"][4]).value == done
+                done += l["grid"][0] * 64
+        assert done == up(cols, 64) * 64 or (done == 0 and len(r["launches"]) == 1), (rows, cols)

@@ -265,3 +265,28 @@ def test_backward_is_the_same_every_time():
         a = _check_backward(300, cols, F32, 64)
         b = _check_backward(300, cols, F32, 64)
         assert all(torch.equal(a[k], b[k]) for k in a)
+
+
+def test_backward_of_more_columns_than_a_launch_holds():
+    """2^28 columns (a dimension of 2^32 threads is cut short without an error) in two runs of one row, which share a gate: small
+    whole numbers in a pattern of 60 columns whose mean(t hn) is zero, so that every sum is exact."""
+    rows, period, cols = 2, 60, 268436400
+    c, r = torch.arange(period)[None], torch.arange(rows)[:, None]
+    dy, h = 1 + (c // 2 + r) % 3, (1 - 2 * (c % 2)).expand(rows, period)  # t hn of columns 2 j and 2 j + 1 cancel
+    dh, u, gate = c % 4 + r, c % 5 - 2 + r, 1 + c % 3
+    H = dh + dy
+    want = {"dpre": (dy * h).sum(0), "dpost": (2 * gate * H * u).sum(0), "dgate": (2 * u * H).sum(0)}  # (gamma_post and r2 are 1, r1 is 2)
+    wide = lambda v: v.to(torch.bfloat16).cuda().repeat(1, cols // period)  # noqa: E731
+    m = {"dy": wide(dy), "dh": wide(dh), "h": wide(h), "u": wide(u), "gate": wide(gate)}
+    ones, r1, r2 = torch.ones(cols, device="cuda"), torch.full((rows,), 2.0, device="cuda"), torch.ones(rows, device="cuda")
+    got = {k: torch.full((cols,), float("nan"), dtype=torch.bfloat16 if k == "dgate" else torch.float32, device="cuda") for k in want}
+    dx, du = torch.empty_like(m["u"]), torch.empty_like(m["u"])
+    ws = torch.empty(perf.perf_residual_norm_backward_workspace_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+    p = {k: v.data_ptr() for k, v in m.items()}
+    perf.perf_residual_norm_backward(p["dy"], p["dh"], p["h"], p["u"], p["gate"], ones.data_ptr(), ones.data_ptr(), r1.data_ptr(),
+                                     r2.data_ptr(), dx.data_ptr(), du.data_ptr(), got["dgate"].data_ptr(), got["dpost"].data_ptr(),
+                                     got["dpre"].data_ptr(), ws.data_ptr(), rows, cols, cols, cols, cols, cols, cols, rows, cols, cols, cols,
+                                     1.0, BF16, BF16, F32, stream=G.stream())
+    for name, v in want.items():
+        assert bool((got[name].view(-1, period) == v.cuda().to(got[name].dtype)).all()), name
+    assert bool((dx.view(rows, -1, period) == H.cuda().to(torch.bfloat16)[:, None]).all())
