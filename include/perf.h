@@ -247,6 +247,8 @@ perf_status perf_quantize_fp8(const void *x, void *q, float *scales, void *qt, f
  * one rounding to c_dt.  Sums are fp32.  For f32 C every product is exact; for bf16 C the matrix instructions, of eight
  * products that they add at once, drop what lies below 2^-13 of the largest (less than 2^-10 of the sum of the products'
  * magnitudes in the worst case, 1e-5 to 4e-5 of C as a rule, where a rounding to bf16 is 4e-3).
+ * A block's sum may be multiplied by scaleA before scaleB, in fp32: with scaleA between 2^-100 and 2^95 (blocks of zeros: any)
+ * that loses nothing, whatever scaleB is; beyond, it may underflow or overflow where the product of all three would not.
  *   A       device, M x K, 8-bit, row stride lda; a_dt E4M3 or E5M2;  scaleA  device fp32, M x ceil(K/128), row stride ldsa
  *   B       device, N x K, 8-bit, row stride ldb; b_dt E4M3;  scaleB  device fp32, ceil(N / b_block_rows) x ceil(K/128), row
  *           stride ldsb; b_block_rows 1 (a scale for 128 elements of a row) or 128 (for a tile)

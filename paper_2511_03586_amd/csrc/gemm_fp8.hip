@@ -41,21 +41,21 @@ struct Gemm8Args {
 template <bool WIDE> struct Fragment { int8v_t v; };
 template <> struct Fragment<true> { bf16x8_t v[4]; };
 
-// Elements 2 w and 2 w + 1 of a fragment's eight from 8 q on as bf16, exactly: one instruction
+// Elements 2 w and 2 w + 1 of a fragment's eight from 8 q on, times a power of two, as bf16, exactly: one instruction
 template <bool E5M2>
-__device__ __forceinline__ void widen_two(Fragment<true> &f, int8v_t v, int q, int w)
+__device__ __forceinline__ void widen_two(Fragment<true> &f, int8v_t v, int q, int w, float power = 1.0f)
 {
     const int src = v[2 * q + (w >> 1)];
     if constexpr (E5M2) {
-        const auto two = (w & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(src, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(src, 1.0f, false);
+        const auto two = (w & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(src, power, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(src, power, false);
         f.v[q][2 * w] = two[0], f.v[q][2 * w + 1] = two[1];
     } else {
-        const auto two = (w & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(src, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(src, 1.0f, false);
+        const auto two = (w & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(src, power, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(src, power, false);
         f.v[q][2 * w] = two[0], f.v[q][2 * w + 1] = two[1];
     }
 }
 template <bool WIDE, bool E5M2>
-__device__ __forceinline__ Fragment<WIDE> as_fragment(int8v_t v)
+__device__ __forceinline__ Fragment<WIDE> as_fragment(int8v_t v, float power = 1.0f)
 {
     Fragment<WIDE> f;
     if constexpr (!WIDE) {
@@ -64,7 +64,7 @@ __device__ __forceinline__ Fragment<WIDE> as_fragment(int8v_t v)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
 #pragma unroll
-            for (int w = 0; w < 4; ++w) widen_two<E5M2>(f, v, q, w);
+            for (int w = 0; w < 4; ++w) widen_two<E5M2>(f, v, q, w, power);
     }
     return f;
 }
@@ -269,8 +269,10 @@ constexpr int tile_lds_bytes(int BM, int BN, int S, int waves) { return S * tile
 // issue holds back the products behind it.
 //
 // The scale of a 128 x 128 tile of B (B128) is the same for all sums of a wave: its exponent goes into the matrix
-// instruction, its mantissa into the factor of A's scale, which leaves one multiply-add per sum, and no product of two
-// scales that could leave fp32's range.
+// instruction (WIDE: into B's elements as they are widened), its mantissa into the factor of A's scale, which leaves one
+// multiply-add per sum, and no product of two scales that could leave fp32's range.  A block's sum is at most 128 x 57344 x 448,
+// less than 2^32: the exponent is taken up to 2^95, down to 2^-60, and what is beyond stays in the factor, which A's scales of
+// up to 2^95 keep finite, and whose product with a sum of 2^-60 underflows only where the result does.
 template <int TM, int TN, int WM, int WN, int S, bool B128, bool A5, typename CT>
 __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Gemm8Args g, int tiles_m, int tiles_n)
 {
@@ -421,10 +423,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Ge
         if constexpr (B128) {
             const uint32_t bits = __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, next128));
             mantissa = __builtin_bit_cast(float, bits);
-            if constexpr (!WIDE) {  // (within 2^60, so that no product of the instruction leaves fp32; the rest stays in the factor)
-                exponent = min(max((int)(bits >> 23 & 0xff), 127 - 60), 127 + 60);
-                mantissa = __builtin_ldexpf(mantissa, 127 - exponent);
-            }
+            exponent = min(max((int)(bits >> 23 & 0xff), 127 - 60), 127 + 95);
+            mantissa = __builtin_ldexpf(mantissa, 127 - exponent);
         }
         Fragment<WIDE> fragment_b[WIDE ? TN : 1];
         if constexpr (MASK) {
@@ -433,7 +433,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Ge
         }
         if constexpr (WIDE) {
 #pragma unroll
-            for (int j = 0; j < TN; ++j) fragment_b[j] = as_fragment<WIDE, false>(b[j]);
+            for (int j = 0; j < TN; ++j) fragment_b[j] = as_fragment<WIDE, false>(b[j], __builtin_bit_cast(float, exponent << 23));
             if constexpr (MASK) a[0] = masked_fragment(a[0], left, lane);
             next_a = as_fragment<WIDE, A5>(a[0]);
         }
