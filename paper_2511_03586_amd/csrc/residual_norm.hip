@@ -602,7 +602,6 @@ __global__ __launch_bounds__(1024) void residual_norm_sums_kernel(const GradArgs
     int64_t step = a.cols;
     if (gamma) {
         if (!(post ? a.dpost : a.dpre)) return;
-        if (!post && !a.has_dy) count = 0;
     } else {
         if (gate >= gates) return;  // (whole waves, and no barrier behind)
         g = by_run ? div_by(min(a.rows, (gate + 1) * a.run) - 1, a.gate_rows, a.gate_magic) : gate;
