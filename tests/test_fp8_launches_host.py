@@ -94,3 +94,24 @@ def test_norm_gradient_sums_of_all_columns_are_launched(recorder):
                 assert ctypes.c_int32(l["args"][4]).value == done
                 done += l["grid"][0] * 64
         assert done == up(cols, 64) * 64 or (done == 0 and len(r["launches"]) == 1), (rows, cols)
+
+
+def _gemm(m, n, k, batch, b_rows, a_dt, c_dt):
+    return ("perf_gemm_fp8", dict(A=FAKE, scaleA=FAKE, B=FAKE, scaleB=FAKE, C=FAKE, M=m, N=n, K=k, lda=up(k, 16) * 16, ldsa=up(k),
+                                  ldb=up(k, 16) * 16, ldsb=up(k), ldc=n, b_block_rows=b_rows, batch=batch, strideC=m * n, a_dt=a_dt,
+                                  c_dt=c_dt))
+
+
+def test_gemm_grids(recorder):
+    """Every product is launched, unless its tiles of 128 x 128 are more than a launch holds: then none is."""
+    extents = (1, 16, 17, 33, 65, 128, 129, 300, 4096, 1 << 16, 1 << 23, (1 << 27) + 1, MOST)
+    calls = [_gemm(m, n, k, batch, b_rows, a_dt, c_dt) for m in extents for n in extents for k in (1, 300, 1500, 8000)
+             for batch in (1, 70000) if m * n * batch <= 1 << 56 for b_rows, a_dt, c_dt in ((1, E4M3, F32), (128, E5M2, BF16), (128, E4M3, F32))]
+    refused = 0
+    for (_, a), r in zip(calls, L.record(recorder, calls)):
+        if r["status"] == perf.PERF_ERR_UNSUPPORTED:
+            assert up(a["M"], 128) * up(a["N"], 128) * 256 >= 1 << 32 and not r["launches"], a
+            refused += 1
+        else:
+            _check_grids([r])
+    assert refused < len(calls) // 4
