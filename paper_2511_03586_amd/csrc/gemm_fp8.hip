@@ -10,9 +10,9 @@
 // by 1.3e-5 of its norm, whatever K).  Below the rounding of a bf16 C, 1.6e-3, that does not show.  For an fp32 C the operands
 // are widened to bf16, exactly, and multiplied by v_mfma_f32_16x16x32_bf16, whose sums are fp32 (3e-8): half the rate.
 //
-//  * gemm_fp8_tile_kernel: operands pass through LDS, two or four stages of one block of K; a workgroup tile of 256 x 256 (bf16 C) or
-//    128 x 128 (fp32 C: or 128 x 96).  Bound by the matrix units at the clock that their power leaves (1.55 to 1.83 GHz) and by the additions
-//    beside them: 4096^3 bf16 C 62 to 67 us (2.1 PFLOP/s), fp32 C 120 us (1.1 PFLOP/s).
+//  * gemm_fp8_tile_kernel: operands pass through LDS, two or four stages of one block of K; a workgroup tile of 256 x 256 (bf16 C)
+//    or 128 x 128 (fp32 C: or 128 x 96).  Bound by the matrix units at the clock that their power leaves (1.55 to 1.83 GHz) and by
+//    the additions beside them: 4096^3 bf16 C 62 to 67 us (2.1 PFLOP/s), fp32 C 120 to 130 us (1.1 PFLOP/s).
 //  * gemm_fp8_waves_kernel: few output tiles or few rows; the waves of a workgroup share one tile and divide the blocks
 //    of K, each with LDS of its own to load through; their sums are added through LDS in the waves' order.  Bound by the
 //    operands' bytes: 64 x 14336 x 4096 14.2 us (4.3 TB/s); 1 x 4096 x 4096 5.4 us, of which half is the launch.
