@@ -312,6 +312,76 @@ perf_status perf_residual_norm_backward(const void *dy, const void *dh, const vo
                                         int64_t lddg, float residual_scale, perf_dtype x_dt, perf_dtype gate_dt,
                                         perf_dtype param_dt, perf_stream stream);
 
+/* A cache of keys and values in 8 bits for a block that serves, filled by perf_cache_append_fp8 and read by
+ * perf_cache_attention_fp8.  It is divided into pages of page_size tokens (a power of two from 16 to 256), and each page and
+ * head has one scale:
+ *   k_pages, v_pages    device, e4m3, [pages][kv_heads][page_size][head_dim], 16-byte aligned; head_dim 64, 128 or 256
+ *   k_scales, v_scales  device bytes, [pages][kv_heads]: a byte b stands for 2^(b - 127), and a value held for its e4m3 value
+ *                       times that; 255 marks a block that took an infinity or a NaN and reads as NaN
+ * Both calls serve a batch of sequences, whose new tokens follow each other in one axis of `tokens` rows:
+ *   cu       device int32[sequences + 1], ascending: sequence s brings the rows from cu[s] to cu[s+1], possibly none
+ *   lengths  device int32[sequences]: tokens that the sequence holds before the call; new token i has position lengths[s] + i
+ *   table    device int32, sequences x table_pages, row stride ldt: position p lies in slot p % page_size of page
+ *            table[s][p / page_size]
+ * Nothing of these is read on the host, so a captured graph serves other lengths and pages on replay.  What they hold never
+ * leads outside the buffers: a column the table does not have, or an entry that is not one of `pages`, is a page that is not
+ * there (not written, its keys not seen), a sequence of negative length or of descending rows brings none, and rows that no
+ * sequence has are left as they were.  (An entry of -1 is the usual mark of a page not given out yet.) */
+
+/* Rotates new queries and keys by their positions and appends keys and values to the cache.  Of each head the first rotary_dim
+ * elements are rotated in pairs, (j, j + rotary_dim/2) or, with interleaved = 1, (2j, 2j+1), by the angle whose cosine c and
+ * sine s the row of their position in `rotation` holds:
+ *     x1' = x1*c - x2*s,   x2' = x2*c + x1*s     (fp32, each product and sum rounded; rotary_dim = 0: none).
+ * For each page and head that takes tokens, keys and values each:
+ *     b = least byte >= 1 with max |x| <= 448 * 2^(b-127) over its new tokens; if tokens lie before them in the page, at least
+ *         its scale, and where b is larger than that what they hold is rounded again to the new one (exact unless it leaves
+ *         the normal e4m3 values);
+ *     new tokens are held as x * 2^(127-b) rounded to nearest even.
+ *   q, q_out  device, tokens x q_heads*head_dim, row strides ldq and ldq_out, x_dt: queries and the rotated ones, rounded
+ *             once; both NULL: none.  q_out may be exactly q (same pointer, same stride)
+ *   k, v      device, tokens x kv_heads*head_dim, row strides ldk and ldv, x_dt (rows of one fused projection will do)
+ *   rotation  device fp32, positions x rotary_dim, rows close: rotary_dim/2 cosines, then as many sines; NULL without rotation
+ * A token whose position `rotation` does not have is not stored and its query is left out; a token whose page is not there is not
+ * stored.  Two sequences of a call must not append to the same page; they may share others.  Slots behind a sequence's last token
+ * are left as they were.
+ * Errors: NULL (k, v, pages, scales, table, lengths, cu; rotation with rotary_dim; one of q and q_out), SHAPE (tokens < 1 or
+ * > 2^28, sequences < 1 or > 2^24, heads < 1 or > 1024, q_heads not a multiple of kv_heads, pages < 1 or > 2^30, table_pages <
+ * 1 or table_pages * page_size > 2^30, ldt or a row stride too small, rotary_dim negative, odd or > head_dim, positions < 1 or
+ * > 2^30 with rotary_dim, interleaved not 0 or 1), DTYPE, ALIGN (pages to 16 bytes, else to the element), UNSUPPORTED
+ * (head_dim or page_size not as above, rotary_dim not a multiple of 16, more work than a launch holds), LAUNCH. */
+perf_status perf_cache_append_fp8(const void *q, const void *k, const void *v, const float *rotation, void *q_out, void *k_pages,
+                                  void *v_pages, uint8_t *k_scales, uint8_t *v_scales, const int32_t *table,
+                                  const int32_t *lengths, const int32_t *cu, int64_t tokens, int64_t sequences, int64_t q_heads,
+                                  int64_t kv_heads, int64_t head_dim, int64_t ldq, int64_t ldk, int64_t ldv, int64_t ldq_out,
+                                  int64_t pages, int64_t page_size, int64_t table_pages, int64_t ldt, int64_t rotary_dim,
+                                  int64_t positions, int interleaved, perf_dtype x_dt, perf_stream stream);
+
+/* Attention of new tokens' queries over the cache that holds their sequences, the new tokens included (append them first).  For
+ * query i of sequence s, at position p = lengths[s] + i, and head h, which reads head h / (q_heads/kv_heads) of the cache, over
+ * the keys j <= p, with a window only those > p - window, whose page is there:
+ *     S_j = scale * q . k_j,   o = sum_j exp(S_j) v_j / sum_j exp(S_j),   lse = log sum_j exp(S_j)   (natural logarithm).
+ * Scores, exponentials and sums are fp32, o is rounded once.  bf16 queries: the weights exp(S_j - max) are rounded to bf16 for
+ * their product with the values (2^-8 of each at most; their sum is taken before).  fp32 queries and weights are split into three bf16, so
+ * that every product counts to 2^-24.  A query that sees no key gets o = 0 and lse = -infinity.
+ *   q, o       device, tokens x q_heads*head_dim, row strides ldq and ldo, x_dt
+ *   lse        device fp32, tokens x q_heads, rows close; or NULL
+ *   workspace  device, at least perf_cache_attention_fp8_workspace_bytes(...) bytes of the same arguments, 16-byte aligned,
+ *              contents are scratch; calls that may run at the same time need one each
+ *   max_tokens the most new tokens that a sequence brings (of one that brings more the first max_tokens are computed)
+ *   window     keys that a query sees at most, itself included; 0 = all
+ * What one block of scale 255 holds may turn every query of its sequence in the call to NaN.
+ * The workspace's size is -1 for arguments that the call would reject.
+ * Errors: NULL (all but lse), SHAPE (as perf_cache_append_fp8; max_tokens < 1, window < 0 or > 2^30, scale not finite), DTYPE,
+ * ALIGN, UNSUPPORTED (head_dim or page_size as above, more work than a launch holds), LAUNCH. */
+int64_t perf_cache_attention_fp8_workspace_bytes(int64_t tokens, int64_t sequences, int64_t max_tokens, int64_t q_heads,
+                                                 int64_t kv_heads, int64_t head_dim, int64_t page_size, int64_t table_pages);
+perf_status perf_cache_attention_fp8(const void *q, const void *k_pages, const void *v_pages, const uint8_t *k_scales,
+                                     const uint8_t *v_scales, const int32_t *table, const int32_t *lengths, const int32_t *cu,
+                                     void *o, float *lse, void *workspace, int64_t tokens, int64_t sequences, int64_t max_tokens,
+                                     int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t ldq, int64_t ldo, int64_t pages,
+                                     int64_t page_size, int64_t table_pages, int64_t ldt, int64_t window, float scale,
+                                     perf_dtype x_dt, perf_stream stream);
+
 /* The same operators with the kernel variant chosen by the caller instead of by the
  * library's shape rules: the knob a timing-driven search turns (the paper's search scores a
  * candidate by the measured runtime of the code it emits, Section 3.2, after validating its

@@ -56,6 +56,9 @@ SIGNATURES = {
     "perf_residual_norm": (_int, [_ptr] * 10 + [_i64] * 9 + [_f32, _f32] + [_int] * 4 + [_ptr]),
     "perf_residual_norm_backward_workspace_bytes": (_i64, [_i64, _i64]),
     "perf_residual_norm_backward": (_int, [_ptr] * 15 + [_i64] * 11 + [_f32, _int, _int, _int, _ptr]),
+    "perf_cache_append_fp8": (_int, [_ptr] * 12 + [_i64] * 15 + [_int, _int, _ptr]),
+    "perf_cache_attention_fp8_workspace_bytes": (_i64, [_i64] * 8),
+    "perf_cache_attention_fp8": (_int, [_ptr] * 11 + [_i64] * 13 + [_f32, _int, _ptr]),
     "perf_copy": (_int, [_ptr, _ptr, _i64, _ptr]),
     "perf_stream_probe": (_int, [_ptr, _ptr, _i64, _int, _int, _int, _i64, _int, _ptr]),
     "perf_mfma_probe": (_int, [_ptr, _i64, _ptr]),
@@ -90,7 +93,8 @@ def lib() -> ctypes.CDLL:
 
 _OPERATORS = ("perf_softmax", "perf_layernorm", "perf_gemm", "perf_gemm_softmax", "perf_conv2d", "perf_rmsnorm", "perf_reduce_mean",
               "perf_reduce_mean_ws", "perf_eltwise", "perf_batchnorm", "perf_batchnorm_static", "perf_copy",
-              "perf_quantize_fp8", "perf_gemm_fp8", "perf_residual_norm", "perf_residual_norm_backward")
+              "perf_quantize_fp8", "perf_gemm_fp8", "perf_residual_norm", "perf_residual_norm_backward", "perf_cache_append_fp8",
+              "perf_cache_attention_fp8")
 
 
 class _Native:
@@ -314,6 +318,33 @@ def perf_residual_norm_backward(dy, dh, h, u, gate, gamma_post, gamma_pre, rrms_
         cols, lddy, lddh, ldh, ldu, ldg, gate_rows, lddx, lddu, lddg, residual_scale, x_dt, gate_dt, param_dt, stream)
     if status and check:
         raise PerfError("perf_residual_norm_backward", status)
+    return status
+
+
+def perf_cache_append_fp8(q, k, v, rotation, q_out, k_pages, v_pages, k_scales, v_scales, table, lengths, cu, tokens, sequences,
+                          q_heads, kv_heads, head_dim, ldq, ldk, ldv, ldq_out, pages, page_size, table_pages, ldt, rotary_dim=0,
+                          positions=0, interleaved=0, x_dt=PERF_BF16, stream=None, check=True) -> int:
+    status = _native.perf_cache_append_fp8(
+        q, k, v, rotation, q_out, k_pages, v_pages, k_scales, v_scales, table, lengths, cu, tokens, sequences, q_heads, kv_heads,
+        head_dim, ldq, ldk, ldv, ldq_out, pages, page_size, table_pages, ldt, rotary_dim, positions, interleaved, x_dt, stream)
+    if status and check:
+        raise PerfError("perf_cache_append_fp8", status)
+    return status
+
+
+def perf_cache_attention_fp8_workspace_bytes(tokens, sequences, max_tokens, q_heads, kv_heads, head_dim, page_size, table_pages) -> int:
+    return int(lib().perf_cache_attention_fp8_workspace_bytes(tokens, sequences, max_tokens, q_heads, kv_heads, head_dim, page_size,
+                                                              table_pages))
+
+
+def perf_cache_attention_fp8(q, k_pages, v_pages, k_scales, v_scales, table, lengths, cu, o, lse, workspace, tokens, sequences,
+                             max_tokens, q_heads, kv_heads, head_dim, ldq, ldo, pages, page_size, table_pages, ldt, window, scale,
+                             x_dt=PERF_BF16, stream=None, check=True) -> int:
+    status = _native.perf_cache_attention_fp8(
+        q, k_pages, v_pages, k_scales, v_scales, table, lengths, cu, o, lse, workspace, tokens, sequences, max_tokens, q_heads,
+        kv_heads, head_dim, ldq, ldo, pages, page_size, table_pages, ldt, window, scale, x_dt, stream)
+    if status and check:
+        raise PerfError("perf_cache_attention_fp8", status)
     return status
 
 

@@ -81,7 +81,8 @@ PyObject *call(const char *name, perf_status (*f)(A...), PyObject *const *args, 
 #define PERF_OPERATORS(X)                                                                                                        \
     X(perf_softmax) X(perf_layernorm) X(perf_gemm) X(perf_gemm_softmax) X(perf_conv2d) X(perf_rmsnorm) X(perf_reduce_mean)       \
     X(perf_reduce_mean_ws) X(perf_eltwise) X(perf_batchnorm) X(perf_batchnorm_static) X(perf_copy)                      \
-    X(perf_quantize_fp8) X(perf_gemm_fp8) X(perf_residual_norm) X(perf_residual_norm_backward)
+    X(perf_quantize_fp8) X(perf_gemm_fp8) X(perf_residual_norm) X(perf_residual_norm_backward) X(perf_cache_append_fp8)          \
+    X(perf_cache_attention_fp8)
 
 #define PERF_METHOD(F)            \
     decltype(&F) p_##F = nullptr; \
