@@ -16,7 +16,6 @@
 //  * gemm_fp8_waves_kernel: few output tiles or few rows; the waves of a workgroup share one tile and divide the blocks
 //    of K, each with LDS of its own to load through; their sums are added through LDS in the waves' order.  Bound by the
 //    operands' bytes: 64 x 14336 x 4096 14.2 us (4.3 TB/s); 1 x 4096 x 4096 5.4 us, of which half is the launch.
-#include <atomic>
 #include "fp8.h"
 #include "mfma_tile.h"
 #include "host_utils.h"
@@ -561,20 +560,6 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gemm_fp8_tile_kernel(const Ge
                 }
         }
     }
-}
-
-// Raises a kernel's limit of dynamic LDS, an idempotent setting, at its first launch on each device.
-template <auto KERNEL>
-static bool allow_lds(int bytes)
-{
-    static std::atomic<uint64_t> done{0};
-    int device = 0;
-    if (hipGetDevice(&device) != hipSuccess) return false;
-    const uint64_t bit = 1ull << (device & 63);
-    if (device < 64 && (done.load(std::memory_order_relaxed) & bit)) return true;
-    if (hipFuncSetAttribute(reinterpret_cast<const void *>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return false;
-    done.fetch_or(bit, std::memory_order_relaxed);
-    return true;
 }
 
 template <int TM, int TN, int WM, int WN, int S, bool A5, typename CT>

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include "../../include/perf.h"
 
@@ -23,6 +24,20 @@ constexpr int64_t kMaxGridX = 2147483647;  // HIP grid.x limit
 constexpr int64_t kMaxGridYZ = 65535;
 // A dimension of 2^32 threads or more is not refused at launch but cut short.
 constexpr int64_t max_blocks(int threads) { return 4294967295LL / threads; }
+
+// Raises a kernel's limit of dynamic LDS, an idempotent setting, at its first launch on each device.
+template <auto KERNEL>
+bool allow_lds(int bytes)
+{
+    static std::atomic<uint64_t> done{0};
+    int device = 0;
+    if (hipGetDevice(&device) != hipSuccess) return false;
+    const uint64_t bit = 1ull << (device & 63);
+    if (device < 64 && (done.load(std::memory_order_relaxed) & bit)) return true;
+    if (hipFuncSetAttribute(reinterpret_cast<const void *>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return false;
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return true;
+}
 
 // Extents of the operators on 8-bit values: indexes of rows, columns and blocks are 32 bits wide in their kernels.
 constexpr int64_t kMaxExtent8 = 1ll << 30;
