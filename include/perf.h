@@ -319,14 +319,15 @@ perf_status perf_residual_norm_backward(const void *dy, const void *dh, const vo
  *   k_scales, v_scales  device bytes, [pages][kv_heads]: a byte b stands for 2^(b - 127), and a value held for its e4m3 value
  *                       times that; 255 marks a block that took an infinity or a NaN and reads as NaN
  * Both calls serve a batch of sequences, whose new tokens follow each other in one axis of `tokens` rows:
- *   cu       device int32[sequences + 1], ascending: sequence s brings the rows from cu[s] to cu[s+1], possibly none
+ *   cu       device int32[sequences + 1], ascending: sequence s brings the rows from cu[s] to cu[s+1], possibly none (where cu
+ *            descends, which rows are computed is not specified)
  *   lengths  device int32[sequences]: tokens that the sequence holds before the call; new token i has position lengths[s] + i
  *   table    device int32, sequences x table_pages, row stride ldt: position p lies in slot p % page_size of page
  *            table[s][p / page_size]
  * Nothing of these is read on the host, so a captured graph serves other lengths and pages on replay.  What they hold never
  * leads outside the buffers: a column the table does not have, or an entry that is not one of `pages`, is a page that is not
- * there (not written, its keys not seen), a sequence of negative length or of descending rows brings none, and rows that no
- * sequence has are left as they were.  (An entry of -1 is the usual mark of a page not given out yet.) */
+ * there (not written, its keys not seen), a sequence of negative length brings none, and rows that no sequence has are left as
+ * they were.  (An entry of -1 is the usual mark of a page not given out yet.) */
 
 /* Rotates new queries and keys by their positions and appends keys and values to the cache.  Of each head the first rotary_dim
  * elements are rotated in pairs, (j, j + rotary_dim/2) or, with interleaved = 1, (2j, 2j+1), by the angle whose cosine c and

@@ -17,9 +17,9 @@ struct AttentionArgs {
     int64_t ldq, ldo;
     int q_heads, kv_heads, max_tokens, window;
     float scale;
-    // scratch: tiles of the few rows' kernel before each sequence, and sums that workgroups leave
-    int64_t *before;
-    float *partial;
+    // scratch of the kernels for few and for many rows: tiles before each sequence or row tile, and the sums that workgroups leave
+    int64_t *few_before, *many_before;
+    float *few_partial, *many_partial;
 };
 
 // Elements d .. d + 3 of a query and head from the sums of weights and of weighted values
@@ -127,6 +127,63 @@ __device__ __forceinline__ Span span(const AttentionArgs &a, int s)
     return r;
 }
 
+// A kernel's tiles, of all items one after the other, are cut into one run for each worker, and none is empty: as many workers as
+// tiles, if those are fewer.  The worker of a tile is the last whose run begins at it or before.
+__device__ __forceinline__ int workers_of(int64_t total, int workers) { return (int)min(total, (int64_t)workers); }
+__device__ __forceinline__ int64_t run_start(int64_t total, int worker, int workers) { return total * worker / workers; }
+__device__ __forceinline__ int worker_of(int64_t total, int64_t tile, int workers) { return (int)(((tile + 1) * workers - 1) / total); }
+
+// Tiles before each of `items` (each thread adds up a run of them) and of all, `copies` times over.  The item in which the run of
+// `worker` begins and the tiles before it are found on the way; `list` receives the tiles before all of them, [items + 1].
+struct Place {
+    int64_t total, start, stop;  // tiles of all copies, and this worker's run of them
+    int64_t before;              // of one copy, before the item
+    int copy, item;
+};
+struct PlaceScratch { int64_t of_wave[4], before, item; };
+template <typename Tiles>
+__device__ __forceinline__ Place find_place(PlaceScratch &at, int items, int copies, int worker, int most, int64_t *list, Tiles &&tiles_of)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int each = (items + 255) / 256, from = min(tid * each, items), to = min(from + each, items);
+    int64_t mine = 0;
+    tiles_of(from, to, [&](int, int n) { mine += n; });
+    int64_t upto = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int64_t v = __shfl_up((long long)upto, d);
+        upto += lane >= d ? v : 0;
+    }
+    if (lane == 63) at.of_wave[wave] = upto;
+    __syncthreads();
+    int64_t one = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        upto += w < wave ? at.of_wave[w] : 0;
+        one += at.of_wave[w];
+    }
+    Place p;
+    p.total = one * copies;
+    const int workers = workers_of(p.total, most);
+    const bool some = worker < workers;
+    p.start = some ? run_start(p.total, worker, workers) : 0;
+    p.stop = some ? run_start(p.total, worker + 1, workers) : 0;
+    p.copy = some ? (int)(p.start / one) : 0;
+    const int64_t x = p.start - p.copy * one;
+    int64_t before = upto - mine;
+    if (list || (some && x >= before && x < upto))
+        tiles_of(from, to, [&](int i, int n) {
+            if (list) list[i] = before;
+            if (x >= before && x < before + n) at.before = before, at.item = i;
+            before += n;
+        });
+    if (list && tid == 0) list[items] = one;
+    __syncthreads();
+    p.before = at.before, p.item = (int)at.item;
+    __syncthreads();
+    return p;
+}
+
 // ---- few rows: up to 16 of (token, head of a group) ---------------------------------------------------------------------
 // Decoding: bound by the bytes of the cache.  The keys of all sequences and heads, in tiles of 128, are one list that is cut into
 // equal runs, a workgroup each, whatever the lengths are; a run that begins or ends inside a head's keys leaves its sums in the
@@ -141,7 +198,7 @@ constexpr int kFewRows = 16, kFewWaves = 4, kFewKeys = 32 * kFewWaves;
 template <int D> constexpr int few_stages() { return D == 64 ? 4 : 2; }
 template <int D> constexpr int few_lds() { return kFewWaves * few_stages<D>() * 64 * D; }
 template <int D> constexpr int few_workers() { return D == 256 ? 256 : 512; }  // as many as are on the chip at a time
-template <int D> constexpr int partial_floats() { return kFewRows * (D + 2); }
+constexpr int partial_floats(int rows, int D) { return rows * (D + 2); }  // sums of a tile of rows, maxima, sums of weights
 
 __device__ __forceinline__ bool is_few(const AttentionArgs &a, int count) { return count * (int64_t)(a.q_heads / a.kv_heads) <= kFewRows; }
 
@@ -152,50 +209,6 @@ __device__ __forceinline__ int few_tiles(const AttentionArgs &a, const Span &r)
     return max((r.end - r.begin + kFewKeys - 1) / kFewKeys, 1);
 }
 
-// The run of a worker begins here, and none is empty: as many workers as tiles, if those are fewer.  The worker of a tile is the
-// last whose run begins at it or before.
-__device__ __forceinline__ int workers_of(int64_t total, int workers) { return (int)min(total, (int64_t)workers); }
-__device__ __forceinline__ int64_t run_start(int64_t total, int worker, int workers) { return total * worker / workers; }
-__device__ __forceinline__ int worker_of(int64_t total, int64_t tile, int workers) { return (int)(((tile + 1) * workers - 1) / total); }
-
-// Tiles before each sequence, and of all of them: a thread adds up a run of sequences.  The sequence that tile `x` lies in and the
-// tiles before it are found on the way; `list` receives all of them, [sequences + 1].
-struct Place { int64_t total, before; int s; };
-__device__ __forceinline__ Place few_place(const AttentionArgs &a, int64_t (&sums)[kFewWaves + 3], int worker, int most, int64_t *list)
-{
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int each = (a.t.sequences + 255) / 256, from = min(tid * each, a.t.sequences), to = min(from + each, a.t.sequences);
-    int64_t mine = 0;
-    for (int s = from; s < to; ++s) mine += (int64_t)few_tiles(a, span(a, s)) * a.kv_heads;
-    int64_t upto = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int64_t v = __shfl_up((long long)upto, d);
-        upto += lane >= d ? v : 0;
-    }
-    if (lane == 63) sums[wave] = upto;
-    __syncthreads();
-    int64_t total = 0;
-#pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) {
-        upto += w < wave ? sums[w] : 0;
-        total += sums[w];
-    }
-    const int workers = workers_of(total, most);
-    const int64_t x = worker < workers ? run_start(total, worker, workers) : total;
-    int64_t before = upto - mine;
-    if (list || (x >= before && x < upto))
-        for (int s = from; s < to; ++s) {
-            const int64_t n = (int64_t)few_tiles(a, span(a, s)) * a.kv_heads;
-            if (list) list[s] = before;
-            if (x >= before && x < before + n) sums[kFewWaves] = before, sums[kFewWaves + 1] = s;
-            before += n;
-        }
-    if (list && tid == 0) list[a.t.sequences] = total;
-    __syncthreads();
-    return Place{total, sums[kFewWaves], (int)sums[kFewWaves + 1]};
-}
-
 template <int D, typename T>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_kernel(const AttentionArgs a)
 {
@@ -204,13 +217,13 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, col = lane & 15;
     const int worker = blockIdx.x, group = a.q_heads / a.kv_heads, shift = a.t.page_shift, in_page = (1 << shift) - 1;
-    int64_t(&sums)[kFewWaves + 3] = *reinterpret_cast<int64_t(*)[kFewWaves + 3]>(smem);
-    const Place place = few_place(a, sums, worker, gridDim.x, worker == 0 ? a.before : nullptr);
-    const int workers = workers_of(place.total, gridDim.x);
-    if (worker >= workers) return;
-    int64_t x = run_start(place.total, worker, workers);
-    const int64_t stop = run_start(place.total, worker + 1, workers);
-    __syncthreads();
+    const Place place = find_place(*reinterpret_cast<PlaceScratch *>(smem), a.t.sequences, 1, worker, gridDim.x,
+                                   worker == 0 ? a.few_before : nullptr, [&](int i, int to, auto &&take) {
+                                       for (; i < to; ++i) take(i, few_tiles(a, span(a, i)) * a.kv_heads);
+                                   });
+    int64_t x = place.start;
+    const int64_t stop = place.stop;
+    if (x >= stop) return;
 
     char *const ring = smem + wave * kStages * kStage;
     // a lane's 16 bytes of load i: row of the block's half and chunk
@@ -224,7 +237,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
     const int v_row = (col >> 1 & 3) + 4 * g + (col >> 3) * 16;
     const float sign = a.scale > 0.f ? 1.f : a.scale < 0.f ? -1.f : 0.f, c = log2_scale(a);
 
-    int s = __builtin_amdgcn_readfirstlane(place.s);
+    int s = __builtin_amdgcn_readfirstlane(place.item);
     Span r = span(a, s);
     int tiles = few_tiles(a, r);
     int head = (int)((x - place.before) / tiles), t0 = (int)((x - place.before) - (int64_t)head * tiles);
@@ -376,7 +389,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
         if (lane < kFewRows) mine[kFewRows * kRow + lane] = m, mine[kFewRows * kRow + kFewRows + lane] = l;
         __syncthreads();
         const bool whole = n == tiles;
-        float *const out = whole ? nullptr : a.partial + (int64_t)(2 * worker + !first) * partial_floats<D>();
+        float *const out = whole ? nullptr : a.few_partial + (int64_t)(2 * worker + !first) * partial_floats(kFewRows, D);
         for (int i = tid; i < rows * (D / 4); i += 256) {
             const int row = i / (D / 4), d = 4 * (i % (D / 4));
             float mw[kFewWaves], top = -INFINITY, sum = 0.f;
@@ -412,145 +425,419 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
     }
 }
 
-// Joins what several workgroups have left of one query and head: in their order, their maxima first.
-template <int D, typename T>
-__global__ __launch_bounds__(256) void cache_attention_join_kernel(const AttentionArgs a, int most)
+// ---- many rows --------------------------------------------------------------------------------------------------------------
+// Prompts: bound by the matrix units and by the vector work beside them.  Tiles of 128 rows of (token, head of a group) and one
+// head of the cache meet its keys 64 at a time, which pass through three stages of LDS, loaded by all four waves, one barrier to a
+// block; each wave has 32 rows.  The blocks of all row tiles and heads are one list, cut into equal runs as above, heads first: an
+// XCD's workgroups take neighbouring runs, which share keys in its L2.
+//
+// The products are those above on v_mfma_f32_32x32x16_bf16: a lane has one query, and keys 4 g .. 4 g + 3 of every eight (g =
+// lane / 32).  The weights of bf16 queries are rounded to bf16 once (the few rows' kernel, which waits for memory, keeps 16 bits
+// of them): another product with what that leaves would cost half of the time again.  A running maximum is raised only by more
+// than 2^8 in weights, which fp32 sums carry as well: the sums are then seldom scaled.
+constexpr int kManyRows = 128, kManyKeys = 64, kManyStages = 3;
+
+template <int D> constexpr int many_lds() { return kManyStages * 2 * kManyKeys * D; }
+// workgroups to a CU: one where a wave needs more than 256 registers (its queries and sums)
+template <int D, typename T> constexpr int many_per_cu() { return D == 256 || (D == 128 && sizeof(T) == 4) ? 1 : 2; }
+template <int D, typename T> constexpr int many_workers() { return 256 * many_per_cu<D, T>(); }
+constexpr int kStartsInLds = 2048;
+
+template <int D> __device__ __forceinline__ constexpr int turn_many_v(int r)
 {
-    constexpr int kLanes = D / 4, kTeams = 256 / kLanes;  // lanes that share a query, and teams that share the workgroups
-    __shared__ float factor[few_workers<D>()], of_wave[2][4];
-    __shared__ float4_t sums[kTeams][kLanes];
-    const int tid = threadIdx.x, token = blockIdx.x / a.q_heads, of_all = blockIdx.x - token * a.q_heads, group = a.q_heads / a.kv_heads;
-    const int s = find_sequence(a.t.sequences, token, [&](int i) { return first_token(a.t, i); });
-    const Span r = span(a, s);
-    const int tiles = few_tiles(a, r);
-    if (token < r.q.first || token >= r.q.first + r.q.count || tiles == 0) return;
-    const int head = of_all / group, row = (token - r.q.first) * group + of_all % group;
-    const int64_t total = a.before[a.t.sequences], start = a.before[s] + (int64_t)head * tiles;
-    const int workers = workers_of(total, most);
-    const int from = worker_of(total, start, workers), count = worker_of(total, start + tiles - 1, workers) - from + 1;
-    if (count == 1) return;
-    const auto partial = [&](int i) {
-        return a.partial + (int64_t)(2 * (from + i) + (run_start(total, from + i, workers) < start)) * partial_floats<D>();
-    };
-    const float c = log2_scale(a);
-    float top = -INFINITY;
-    for (int i = tid; i < count; i += 256) {
-        factor[i] = partial(i)[kFewRows * D + row];
-        top = __builtin_fmaxf(top, factor[i]);
-    }
-    top = wave_allreduce(top, OpMax());
-    if ((tid & 63) == 0) of_wave[0][tid >> 6] = top;
-    __syncthreads();
-    top = __builtin_fmaxf(__builtin_fmaxf(of_wave[0][0], of_wave[0][1]), __builtin_fmaxf(of_wave[0][2], of_wave[0][3]));
-    const float top_c = top == -INFINITY ? 0.f : top * c;
-    float sum = 0.f;
-    for (int i = tid; i < count; i += 256) {
-        factor[i] = weight(factor[i], c, top_c);
-        sum += factor[i] * partial(i)[kFewRows * (D + 1) + row];
-    }
-    sum = wave_allreduce(sum, OpSum());
-    if ((tid & 63) == 0) of_wave[1][tid >> 6] = sum;
-    __syncthreads();
-    sum = (of_wave[1][0] + of_wave[1][1]) + (of_wave[1][2] + of_wave[1][3]);
-    const int d = tid % kLanes, team = tid / kLanes;
-    float4_t v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int i = team; i < count; i += kTeams) v += factor[i] * *reinterpret_cast<const float4_t *>(partial(i) + row * D + 4 * d);
-    sums[team][d] = v;
-    __syncthreads();
-    if (team == 0) {
-#pragma unroll
-        for (int i = 1; i < kTeams; ++i) v += sums[i][d];
-        finish<T>(a, token, of_all, 4 * d, D, v, top, sum);
-    }
+    return D == 64 ? (((r >> 3) & 1) << 1) | ((r >> 2) & 1) : D == 128 ? (((r >> 1) & 1) << 1) | (((r >> 3) & 1) << 2) | ((r >> 2) & 1) : ((r & 3) << 1) | (((r >> 3) & 1) << 3) | ((r >> 2) & 1);
 }
 
-// One workgroup for a query and head: keys 256 at a time, one a thread; values an element a thread.
-template <int D, typename T>
-__global__ __launch_bounds__(256) void cache_attention_kernel(const AttentionArgs a)
+// Row tiles of a sequence begin at this number: those of `count` tokens are at most count * group / 128 + 1.
+// (Where cu does not ascend they overlap or leave gaps: then some rows are not computed, and nothing below relies on their order.)
+__device__ __forceinline__ int many_start(const AttentionArgs &a, int s)
 {
-    __shared__ float q[D], p[256], of_wave[4], part[256];
-    const int tid = threadIdx.x;
-    const int token = blockIdx.x / a.q_heads, head = blockIdx.x - token * a.q_heads, kv = head / (a.q_heads / a.kv_heads);
-    const int s = find_sequence(a.t.sequences, token, [&](int i) { return first_token(a.t, i); });
-    Sequence seq = sequence(a.t, s);
-    seq.count = min(seq.count, a.max_tokens);
-    if (token < seq.first || token >= seq.first + seq.count || is_few(a, seq.count)) return;
-    const int position = seq.held + token - seq.first, shift = a.t.page_shift;
-    const int end = (int)min((int64_t)position + 1, (int64_t)a.t.columns << shift);
-    const int begin = a.window ? max(position - a.window + 1, 0) : 0;
-    if (tid < D) q[tid] = Elem<T>::load1(reinterpret_cast<const T *>(a.q) + token * a.ldq + head * D + tid) * a.scale;
-    __syncthreads();
-    constexpr int kParts = 256 / D;  // threads that share an element
-    const int d = tid % D, mine = tid / D;
-    float m = -INFINITY, l = 0.f, acc = 0.f;
-    for (int from = begin; from < end; from += 256) {
-        const int j = from + tid, page = j < end ? page_at(a.t, s, j >> shift) : -1;
-        float v = -INFINITY;
-        if (page >= 0) {
-            const int64_t block = (int64_t)page * a.kv_heads + kv;
-            const uint8_t *row = a.k_pages + ((block << shift) + (j & ((1 << shift) - 1))) * D;
-            float sum = 0.f;
-            for (int c = 0; c < D; c += 16) {
-                const uint4_t w = *reinterpret_cast<const uint4_t *>(row + c);
+    return s == 0 ? 0 : (int)((int64_t)first_token(a.t, s) * (a.q_heads / a.kv_heads) / kManyRows) + s;
+}
+inline int64_t many_units(int64_t tokens, int64_t sequences, int64_t group) { return tokens * group / kManyRows + sequences; }
+
+// The keys that a row tile needs: [begin, end), begin on a border of 64
+struct Keys { int begin, end, tiles; };
+__device__ __forceinline__ Keys many_keys(const AttentionArgs &a, const Span &r, int tile)
+{
+    const int group = a.q_heads / a.kv_heads, rows = r.q.count * group, row = tile * kManyRows;
+    Keys k{0, 0, 0};
+    if (row >= rows || is_few(a, r.q.count)) return k;
+    const int token0 = row / group, token1 = min(row + kManyRows, rows) - 1;
+    k.end = (int)min((int64_t)r.q.held + token1 / group + 1, (int64_t)a.t.columns << a.t.page_shift);
+    k.begin = a.window ? max(r.q.held + token0 - a.window + 1, 0) & ~(kManyKeys - 1) : 0;
+    k.tiles = max((k.end - k.begin + kManyKeys - 1) / kManyKeys, 1);
+    return k;
+}
+
+template <int D, typename T>
+__global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_many_kernel(const AttentionArgs a, int units)
+{
+    constexpr int kStage = 2 * kManyKeys * D, kLoads = D / 32;                  // loads of a wave and block: K, then V
+    constexpr int kQ = sizeof(T) == 4 ? 3 : 1, kP = sizeof(T) == 4 ? 3 : 1;     // bf16 parts of a query's element and of a weight
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, col = lane & 31;
+    const int group = a.q_heads / a.kv_heads, shift = a.t.page_shift, in_page = (1 << shift) - 1;
+    const int worker = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);  // (a multiple of 8 workgroups)
+
+    // first tokens of the sequences, where they fit
+    int *const starts = reinterpret_cast<int *>(smem + sizeof(PlaceScratch));
+    const bool in_lds = a.t.sequences <= kStartsInLds;
+    if (in_lds) {
+        for (int i = tid; i < a.t.sequences; i += 256) starts[i] = many_start(a, i);
+        __syncthreads();
+    }
+    const auto start_of = [&](int s) { return in_lds ? starts[s] : many_start(a, s); };
+    const Place place = find_place(*reinterpret_cast<PlaceScratch *>(smem), units, a.kv_heads, worker, gridDim.x, worker == 0 ? a.many_before : nullptr,
+                                   [&](int u, int to, auto &&take) {
+                                       int s = 0;  // the last sequence that begins at u or before
+                                       for (int n = a.t.sequences; n > 1;) {
+                                           const int half = n >> 1;
+                                           if (start_of(s + half) <= u) s += half, n -= half; else n = half;
+                                       }
+                                       for (; u < to; ++u) {
+                                           while (s + 1 < a.t.sequences && start_of(s + 1) <= u) ++s;
+                                           take(u, many_keys(a, span(a, s), u - start_of(s)).tiles);
+                                       }
+                                   });
+    int64_t x = place.start;
+    const int64_t stop = place.stop;
+    if (x >= stop) return;
+
+    // a lane's 16 bytes of load i of its wave's 16 rows
+    uint32_t off_k[kLoads / 2], off_v[kLoads / 2];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float k[4];
-                    unpack_e4m3(w[e], k);
+    for (int i = 0; i < kLoads / 2; ++i) {
+        const int row = (i * 64 + lane) / (D / 16), at = lane % (D / 16);
+        off_k[i] = row * D + ((at ^ turn_k<D>(row + 16 * wave)) << 4);
+        off_v[i] = row * D + ((at ^ turn_many_v<D>(row + 16 * wave)) << 4);
+    }
+    const int v_row = 4 * g + (lane >> 1 & 3) + (lane >> 3 & 1) * 8;
+    const float sign = a.scale > 0.f ? 1.f : a.scale < 0.f ? -1.f : 0.f, c = log2_scale(a);
+
+    int head = __builtin_amdgcn_readfirstlane(place.copy), u = __builtin_amdgcn_readfirstlane(place.item);
+    int s = find_sequence(a.t.sequences, u, [&](int i) { return many_start(a, i); });
+    Span r = span(a, s);
+    int tile = u - many_start(a, s);
+    int t0 = (int)(x - head * (place.total / a.kv_heads) - place.before);
+    bool first = true;
+    while (true) {
+        const Keys keys = many_keys(a, r, tile);
+        const int n = (int)min((int64_t)(keys.tiles - t0), stop - x), rows = r.q.count * group;
+        if (n < 1) return;  // (only where cu does not ascend)
+        const int held = __builtin_amdgcn_readfirstlane(r.q.held), end = __builtin_amdgcn_readfirstlane(keys.end);
+        const int from = __builtin_amdgcn_readfirstlane(keys.begin) + t0 * kManyKeys;
+        const int row0 = tile * kManyRows + 32 * wave, row = row0 + col;  // this wave's first row, and this lane's
+        const int token = min(row, rows - 1) / group, of_group = min(row, rows - 1) - token * group, position = held + token;
+        // positions of the wave's first and last row, by which its blocks are taken, masked or left out
+        const int low = __builtin_amdgcn_readfirstlane(position), high = __builtin_amdgcn_readlane(position, 31);
+        const bool active = row0 < rows;
+
+        bf16x8_t q[D / 16][kQ];
+        {
+            const T *in = reinterpret_cast<const T *>(a.q) + (int64_t)(r.q.first + token) * a.ldq + (int64_t)(head * group + of_group) * D;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sum = fmaf(q[c + 4 * e + i], k[i], sum);
+            for (int i = 0; i < D / 16; ++i) {
+                Eight<T> raw;
+                raw.load_cached(in + 32 * (i >> 1) + 16 * g + 8 * (i & 1), 8);
+                float v[8];
+                raw.get(v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] *= sign;
+                split_eight(v, q[i]);
+            }
+        }
+
+        // Pages and scales of 64 pieces of 16 keys, one a lane: 16 blocks
+        int page = -1;
+        uint32_t scales = 0;  // bytes of K and V; bit 16: the page is there
+        auto look_up = [&](int i) {
+            const int k = from + i * kManyKeys + 16 * lane;
+            page = k < end ? page_at(a.t, s, k >> shift) : -1;
+            uint32_t b0 = 0, b1 = 0;
+            if (page >= 0) b0 = a.k_scales[(int64_t)page * a.kv_heads + head], b1 = a.v_scales[(int64_t)page * a.kv_heads + head];
+            scales = b0 | b1 << 8 | (page >= 0 ? 0x10000 : 0);
+            wait_vmem<0>();
+            asm volatile("" : "+v"(page), "+v"(scales));
+        };
+        struct Block { uint32_t scales[4]; };
+        auto issue = [&](int i) {
+            if ((i & 15) == 0) look_up(i);
+            const int piece = 4 * (i & 15), p = __builtin_amdgcn_readlane(page, piece + wave);
+            const rsrc_t in_k = block_rsrc(a.k_pages, a, p, head, D), in_v = block_rsrc(a.v_pages, a, p, head, D);
+            const uint32_t at = (uint32_t)((from + i * kManyKeys + 16 * wave) & in_page) * D;
+            char *const to = smem + (i % kManyStages) * kStage + wave * 16 * D;
+#pragma unroll
+            for (int j = 0; j < kLoads / 2; ++j) issue_load_to(in_k, off_k[j], at, to + j * 1024);
+#pragma unroll
+            for (int j = 0; j < kLoads / 2; ++j) issue_load_to(in_v, off_v[j], at, to + kManyKeys * D + j * 1024);
+            Block b;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b.scales[j] = (uint32_t)__builtin_amdgcn_readlane((int)scales, piece + j);
+            return b;
+        };
+
+        float16_t o[D / 32];
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) o[d] = float16_t{};
+        float m = -INFINITY, l = 0.f;
+        Block ahead[kManyStages];
+        ahead[0] = issue(0);
+        ahead[1] = issue(1);
+        for (int i = 0; i < n; ++i) {
+            wait_vmem<kLoads>();  // this wave's part of the block has arrived, and what it read of the one before
+            wait_lds();
+            wg_barrier();
+            ahead[2] = issue(i + 2);
+            const Block now = ahead[0];
+            ahead[0] = ahead[1], ahead[1] = ahead[2];
+            const int k = from + i * kManyKeys;
+            if (!active || k > high || (a.window && k + kManyKeys - 1 <= low - a.window)) continue;
+            const char *const in_k = smem + (i % kManyStages) * kStage, *const in_v = in_k + kManyKeys * D;
+
+            float16_t sc[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float power = scale_of((col < 16 ? now.scales[2 * h] : now.scales[2 * h + 1]) & 255);
+                const int at = 32 * h + col;
+                sc[h] = float16_t{};
+#pragma unroll
+                for (int j = 0; j < D / 32; ++j) {
+                    const int4v_t w = *reinterpret_cast<const int4v_t *>(in_k + at * D + (((2 * j + g) ^ turn_k<D>(at)) << 4));
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const bf16x8_t f = widen_eight(w[2 * e], w[2 * e + 1], power, power);
+#pragma unroll
+                        for (int p = kQ - 1; p >= 0; --p) sc[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, q[2 * j + e][p], sc[h], 0, 0, 0);
+                    }
                 }
             }
-            v = sum * scale_of(a.k_scales[block]);
-        }
-        float top = wave_allreduce(v, OpMax());
-        if ((tid & 63) == 0) of_wave[tid >> 6] = top;
-        __syncthreads();
-        top = fmaxf(fmaxf(of_wave[0], of_wave[1]), fmaxf(of_wave[2], of_wave[3]));
-        const float next = fmaxf(m, top), keep = next == -INFINITY ? 1.f : expf(m - next);
-        p[tid] = page >= 0 ? expf(v - next) : 0.f;
-        l = l * keep + p[tid];
-        acc *= keep;
-        m = next;
-        __syncthreads();
-        for (int i = mine; i < min(256, end - from); i += kParts) {
-            const int at = from + i, vp = page_at(a.t, s, at >> shift);
-            if (vp < 0) continue;
-            const int64_t block = (int64_t)vp * a.kv_heads + kv;
-            float v4[4];
-            unpack_e4m3(a.v_pages[((block << shift) + (at & ((1 << shift) - 1))) * D + d], v4);
-            acc = fmaf(p[i], v4[0] * scale_of(a.v_scales[block]), acc);
-        }
-        __syncthreads();
-    }
-    l = wave_allreduce(l, OpSum());
-    if ((tid & 63) == 0) of_wave[tid >> 6] = l;
-    part[tid] = acc;
-    __syncthreads();
-    l = of_wave[0] + of_wave[1] + of_wave[2] + of_wave[3];
-    if (tid < D) {
-        float o = 0.f;
+            const bool all_there = (now.scales[0] & now.scales[1] & now.scales[2] & now.scales[3]) >> 16;
+            const bool edge = !all_there || k + kManyKeys - 1 > low || (a.window && k <= high - a.window);
+            if (edge) {
 #pragma unroll
-        for (int i = 0; i < kParts; ++i) o += part[i * D + tid];
-        Elem<T>::store1(reinterpret_cast<T *>(a.o) + token * a.ldo + head * D + tid, l == 0.f ? 0.f : o / l);
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int key = k + 32 * h + 8 * (e >> 2) + 4 * g + (e & 3);
+                        const bool seen = (now.scales[2 * h + (e >> 3)] >> 16) && key < end && key <= position && (!a.window || key > position - a.window);
+                        sc[h][e] = seen ? sc[h][e] : -INFINITY;
+                    }
+            }
+            float top = sc[0][0];
+#pragma unroll
+            for (int e = 1; e < 32; ++e) top = __builtin_fmaxf(top, sc[e >> 4][e & 15]);
+            float t_a, t_b;
+            swap32(top, t_a, t_b);
+            top = __builtin_fmaxf(t_a, t_b);
+            if (__ballot((top - m) * c > 8.f)) {  // (false for two infinities of the same sign)
+                const float next = __builtin_fmaxf(m, top);
+                const float shrink = weight(m, c, next == -INFINITY ? 0.f : next * c);
+                l *= shrink;
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[d][e] *= shrink;
+                m = next;
+            }
+            const float top_c = m == -INFINITY ? 0.f : m * c;
+#pragma unroll
+            for (int step = 0; step < 4; ++step) {
+                float p[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) p[e] = weight(sc[step >> 1][8 * (step & 1) + e], c, top_c);
+                l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+                bf16x8_t w[kP];
+                split_eight(p, w);
+                const float power = scale_of(now.scales[step] >> 8 & 255);
+                int keep[2] = {-1, -1};  // bytes of V that are keys
+                if (edge) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int left = (now.scales[step] >> 16) ? end - (k + 16 * step + 8 * h + 4 * g) : 0;
+                        keep[h] = left >= 4 ? -1 : left <= 0 ? 0 : (1 << (8 * left)) - 1;
+                    }
+                }
+                const int at = 16 * step + v_row;
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d) {
+                    const int2v_t v = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                        (__attribute__((address_space(3))) int2v_t *)(in_v + at * D + (((2 * d + (lane >> 4 & 1)) ^ turn_many_v<D>(at)) << 4) + (lane & 1) * 8));
+                    const bf16x8_t f = widen_eight(v[0] & keep[0], v[1] & keep[1], power, power);
+#pragma unroll
+                    for (int e = kP - 1; e >= 0; --e) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, w[e], o[d], 0, 0, 0);
+                }
+            }
+        }
+        wait_vmem_and_lds<0>();
+        wg_barrier();  // the stages are free
+
+        float l_a, l_b;
+        swap32(l, l_a, l_b);
+        l = l_a + l_b;
+        const bool whole = n == keys.tiles;
+        if (row < rows) {
+            float *const out = whole ? nullptr : a.many_partial + (int64_t)(2 * worker + !first) * partial_floats(kManyRows, D);
+            const int in_tile = 32 * wave + col;
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float4_t v = {o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]};
+                    const int at = 32 * d + 8 * e + 4 * g;
+                    if (whole)
+                        finish<T>(a, r.q.first + token, head * group + of_group, at, D, v, m, l);
+                    else
+                        *reinterpret_cast<float4_t *>(out + in_tile * D + at) = v;
+                }
+            if (!whole && g == 0) out[kManyRows * D + in_tile] = m, out[kManyRows * (D + 1) + in_tile] = l;
+        }
+        first = false;
+        x += n, t0 = 0;
+        if (x >= stop) break;
+        // the next row tile that has keys
+        do {
+            if (++u == units) {
+                u = 0, s = 0;
+                if (++head == a.kv_heads) return;  // (only where cu does not ascend)
+                r = span(a, s);
+            }
+            while (s + 1 < a.t.sequences && many_start(a, s + 1) <= u) r = span(a, ++s);
+            tile = u - many_start(a, s);
+        } while (many_keys(a, r, tile).tiles == 0);
     }
-    if (a.lse && tid == 0) a.lse[(int64_t)token * a.q_heads + head] = m + logf(l);
 }
 
-// Scratch in bytes: tiles before each sequence, then the few rows' sums
-static int64_t list_bytes(int64_t sequences) { return (8 * (sequences + 1) + 15) / 16 * 16; }
-template <int D> static int64_t scratch(int64_t sequences) { return list_bytes(sequences) + 8ll * few_workers<D>() * partial_floats<D>(); }
+// ---- both ----------------------------------------------------------------------------------------------------------------------
+// Joins what several workgroups have left of one tile of rows, in their order, the largest maximum first.  Only a tile that the
+// beginning of a run cuts was divided: a workgroup for each such beginning (the first in its tile) and kRows rows.  What few
+// workgroups left is added by the threads of a row; of more, all teams of D / 4 lanes take a share.
+template <int D, typename T, bool MANY>
+__global__ __launch_bounds__(256) void cache_attention_join_kernel(const AttentionArgs a, int units)
+{
+    constexpr int kRows = MANY ? 8 : 1, kTile = MANY ? kManyRows : kFewRows, kWorkers = MANY ? many_workers<D, T>() : few_workers<D>();
+    constexpr int kLanes = D / 4, kTeams = 256 / kLanes, kSerial = 8;
+    __shared__ float factor[kWorkers], of_wave[2][4];
+    __shared__ float4_t sums[kTeams][kLanes];
+    const int tid = threadIdx.x, worker = blockIdx.x, group = a.q_heads / a.kv_heads, items = MANY ? units : a.t.sequences;
+    const int64_t *const before = MANY ? a.many_before : a.few_before;
+    const float *const partials = MANY ? a.many_partial : a.few_partial;
+    const int64_t one = before[items], total = MANY ? one * a.kv_heads : one;
+    const int workers = workers_of(total, kWorkers);
+    if (worker == 0 || worker >= workers) return;
+    const int64_t x = run_start(total, worker, workers), copy = MANY ? x / one : 0, in_copy = x - copy * one;
+    const int item = find_sequence(items, 0, [&](int i) { return before[i] <= in_copy ? 0 : 1; });
+    int s = item, tile = 0, head, tiles;
+    int64_t start;
+    Span r;
+    if constexpr (MANY) {
+        s = find_sequence(a.t.sequences, item, [&](int i) { return many_start(a, i); });
+        r = span(a, s), tile = item - many_start(a, s), head = (int)copy, start = copy * one + before[item];
+        tiles = many_keys(a, r, tile).tiles;
+    } else {
+        r = span(a, s);
+        tiles = few_tiles(a, r);
+        head = (int)((x - before[item]) / max(tiles, 1)), start = before[item] + (int64_t)head * tiles;
+    }
+    if (start >= x || start < run_start(total, worker - 1, workers) || start + tiles > total) return;
+    const int from = worker - 1, count = worker_of(total, start + tiles - 1, workers) - from + 1;
+    const int rows = min(r.q.count * group - tile * kTile, kTile);
+    const auto partial = [&](int i) {
+        return partials + (int64_t)(2 * (from + i) + (i == 0 && run_start(total, from, workers) < start)) * partial_floats(kTile, D);
+    };
+    const float c = log2_scale(a);
+    const int d = tid % kLanes, team = tid / kLanes;
+    const auto put = [&](int row, float4_t v, float top, float sum) {
+        const int of_all = tile * kTile + row, token = of_all / group;
+        finish<T>(a, r.q.first + token, head * group + of_all - token * group, 4 * d, D, v, top, sum);
+    };
+    if (count <= kSerial) {
+        for (int row = blockIdx.y * kRows + team; row < min((int)(blockIdx.y + 1) * kRows, rows); row += kTeams) {
+            float m[kSerial], l[kSerial], top = -INFINITY, sum = 0.f;
+            float4_t o[kSerial];
+#pragma unroll
+            for (int i = 0; i < kSerial; ++i) {
+                const float *const of = partial(min(i, count - 1));
+                m[i] = of[kTile * D + row], l[i] = of[kTile * (D + 1) + row], o[i] = *reinterpret_cast<const float4_t *>(of + row * D + 4 * d);
+                top = __builtin_fmaxf(top, m[i]);
+            }
+            const float top_c = top == -INFINITY ? 0.f : top * c;
+            float4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < kSerial; ++i)
+                if (i < count) {
+                    const float f = weight(m[i], c, top_c);
+                    v += f * o[i], sum += f * l[i];
+                }
+            put(row, v, top, sum);
+        }
+        return;
+    }
+    for (int row = blockIdx.y * kRows; row < min((int)(blockIdx.y + 1) * kRows, rows); ++row) {
+        float top = -INFINITY;
+        for (int i = tid; i < count; i += 256) {
+            factor[i] = partial(i)[kTile * D + row];
+            top = __builtin_fmaxf(top, factor[i]);
+        }
+        top = wave_allreduce(top, OpMax());
+        if ((tid & 63) == 0) of_wave[0][tid >> 6] = top;
+        __syncthreads();
+        top = __builtin_fmaxf(__builtin_fmaxf(of_wave[0][0], of_wave[0][1]), __builtin_fmaxf(of_wave[0][2], of_wave[0][3]));
+        const float top_c = top == -INFINITY ? 0.f : top * c;
+        float sum = 0.f;
+        for (int i = tid; i < count; i += 256) {
+            factor[i] = weight(factor[i], c, top_c);
+            sum += factor[i] * partial(i)[kTile * (D + 1) + row];
+        }
+        sum = wave_allreduce(sum, OpSum());
+        if ((tid & 63) == 0) of_wave[1][tid >> 6] = sum;
+        __syncthreads();
+        sum = (of_wave[1][0] + of_wave[1][1]) + (of_wave[1][2] + of_wave[1][3]);
+        float4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int i = team; i < count; i += kTeams) v += factor[i] * *reinterpret_cast<const float4_t *>(partial(i) + row * D + 4 * d);
+        sums[team][d] = v;
+        __syncthreads();
+        if (team == 0) {
+#pragma unroll
+            for (int i = 1; i < kTeams; ++i) v += sums[i][d];
+            put(row, v, top, sum);
+        }
+        __syncthreads();
+    }
+}
+
+// Scratch: tiles before each sequence and row tile, then the sums
+struct Scratch { int64_t many_before, few_partial, many_partial, bytes; };  // where these begin, in bytes
+template <int D, typename T>
+static Scratch scratch(int64_t tokens, int64_t sequences, int64_t max_tokens, int64_t group)
+{
+    const bool many = std::min(max_tokens, tokens) * group > kFewRows;
+    Scratch s;
+    s.many_before = 8 * (sequences + 1);
+    s.few_partial = (s.many_before + (many ? 8 * (many_units(tokens, sequences, group) + 1) : 0) + 15) / 16 * 16;
+    s.many_partial = s.few_partial + 8ll * few_workers<D>() * partial_floats(kFewRows, D);
+    s.bytes = s.many_partial + (many ? 8ll * many_workers<D, T>() * partial_floats(kManyRows, D) : 0);
+    return s;
+}
 
 template <int D, typename T>
-static perf_status attention(const AttentionArgs &a, hipStream_t st)
+static perf_status attention(AttentionArgs &a, char *workspace, hipStream_t st)
 {
-    const int64_t group = a.q_heads / a.kv_heads, rows = (int64_t)a.t.tokens * a.q_heads;
-    if (rows > max_blocks(256)) return PERF_ERR_UNSUPPORTED;
+    const int64_t group = a.q_heads / a.kv_heads, units = many_units(a.t.tokens, a.t.sequences, group);
+    if (units > INT32_MAX) return PERF_ERR_UNSUPPORTED;
+    const Scratch at = scratch<D, T>(a.t.tokens, a.t.sequences, a.max_tokens, group);
+    a.few_before = (int64_t *)workspace, a.many_before = (int64_t *)(workspace + at.many_before);
+    a.few_partial = (float *)(workspace + at.few_partial), a.many_partial = (float *)(workspace + at.many_partial);
     const bool many = a.max_tokens * group > kFewRows;  // (whether a sequence of as many tokens is for the other kernel)
     if (!allow_lds<cache_attention_few_kernel<D, T>>(few_lds<D>())) return PERF_ERR_LAUNCH;
     cache_attention_few_kernel<D, T><<<few_workers<D>(), 256, few_lds<D>(), st>>>(a);
-    cache_attention_join_kernel<D, T><<<(uint32_t)rows, 256, 0, st>>>(a, few_workers<D>());
-    if (many) cache_attention_kernel<D, T><<<(uint32_t)rows, 256, 0, st>>>(a);
+    cache_attention_join_kernel<D, T, false><<<dim3(few_workers<D>(), (uint32_t)std::min<int64_t>(kFewRows, a.max_tokens * group)), 256, 0, st>>>(a, (int)units);
+    if (many) {
+        if (!allow_lds<cache_attention_many_kernel<D, T>>(many_lds<D>())) return PERF_ERR_LAUNCH;
+        cache_attention_many_kernel<D, T><<<many_workers<D, T>(), 256, many_lds<D>(), st>>>(a, (int)units);
+        cache_attention_join_kernel<D, T, true><<<dim3(many_workers<D, T>(), kManyRows / 8), 256, 0, st>>>(a, (int)units);
+    }
     return launch_status();
 }
 
@@ -568,7 +855,12 @@ extern "C" int64_t perf_cache_attention_fp8_workspace_bytes(int64_t tokens, int6
 {
     const CacheShape c{tokens, sequences, q_heads, kv_heads, head_dim, 1, page_size, table_pages, table_pages};
     if (!attention_shape_ok(c, max_tokens) || !cache_supported(c)) return -1;
-    return head_dim == 64 ? scratch<64>(sequences) : head_dim == 128 ? scratch<128>(sequences) : scratch<256>(sequences);
+    const int64_t group = q_heads / kv_heads;
+    // (bf16 queries: no type needs more)
+    return (head_dim == 64    ? scratch<64, uint16_t>(tokens, sequences, max_tokens, group)
+            : head_dim == 128 ? scratch<128, uint16_t>(tokens, sequences, max_tokens, group)
+                              : scratch<256, uint16_t>(tokens, sequences, max_tokens, group))
+        .bytes;
 }
 
 extern "C" perf_status perf_cache_attention_fp8(const void *q, const void *k_pages, const void *v_pages, const uint8_t *k_scales,
@@ -594,11 +886,11 @@ extern "C" perf_status perf_cache_attention_fp8(const void *q, const void *k_pag
     a.q = q, a.o = o, a.lse = lse, a.ldq = ldq, a.ldo = ldo;
     a.k_pages = (const uint8_t *)k_pages, a.v_pages = (const uint8_t *)v_pages, a.k_scales = k_scales, a.v_scales = v_scales;
     a.q_heads = (int)q_heads, a.kv_heads = (int)kv_heads, a.max_tokens = (int)std::min(max_tokens, tokens), a.window = (int)window, a.scale = scale;
-    a.before = (int64_t *)workspace, a.partial = (float *)((char *)workspace + list_bytes(sequences));
     const hipStream_t st = (hipStream_t)stream;
     const auto with = [&](auto one) {
         using T = decltype(one);
-        return head_dim == 64 ? attention<64, T>(a, st) : head_dim == 128 ? attention<128, T>(a, st) : attention<256, T>(a, st);
+        char *const ws = (char *)workspace;
+        return head_dim == 64 ? attention<64, T>(a, ws, st) : head_dim == 128 ? attention<128, T>(a, ws, st) : attention<256, T>(a, ws, st);
     };
     return x_dt == PERF_BF16 ? with(uint16_t{}) : with(float{});
 }

@@ -105,7 +105,7 @@ def test_append_beyond_the_table():
 
 
 def test_append_bad_lengths_and_rows():
-    """A sequence of negative length, and one whose rows descend, bring nothing; the others are served."""
+    """A sequence of negative length brings nothing; the others are served."""
     batch = C.Batch([5, 6, 7], [4, 4, 4], 16, 1)
     cache = C.Cache(batch.pages, 1, 16, 64)
     C.fill(cache, batch, 2, upto_new=False)
