@@ -67,6 +67,13 @@ __device__ __forceinline__ void split_eight(const float (&x)[8], bf16x8_t (&part
     }
 }
 
+// Values that are the same in all lanes, in scalar registers
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform(int64_t v)
+{
+    return (int64_t)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
+}
+
 // All of this wave's LDS accesses are done; its loads stay in flight.
 __device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xC07F); }
 __device__ __forceinline__ void fence() { asm volatile("" ::: "memory"); }
@@ -108,7 +115,8 @@ template <int D> __device__ __forceinline__ constexpr int turn_v(int r)
 
 __device__ __forceinline__ rsrc_t block_rsrc(const uint8_t *pages, const AttentionArgs &a, int page, int head, int D)
 {
-    const int64_t block = (int64_t)max(page, 0) * a.kv_heads + head;
+    // (64-bit products are made in vector registers, and a resource that lies there is read lane by lane)
+    const int64_t block = uniform((int64_t)max(page, 0) * a.kv_heads + head);
     return make_rsrc(pages + (block << a.t.page_shift) * D, page < 0 ? 0 : (uint32_t)D << a.t.page_shift);
 }
 
@@ -125,6 +133,10 @@ __device__ __forceinline__ Span span(const AttentionArgs &a, int s)
     r.end = (int)min((int64_t)r.q.held + r.q.count, (int64_t)a.t.columns << a.t.page_shift);
     r.begin = a.window ? max(r.q.held - a.window + 1, 0) & ~31 : 0;
     return r;
+}
+__device__ __forceinline__ Span uniform(Span r)
+{
+    return Span{Sequence{uniform(r.q.first), uniform(r.q.count), uniform(r.q.held)}, uniform(r.begin), uniform(r.end)};
 }
 
 // A kernel's tiles, of all items one after the other, are cut into one run for each worker, and none is empty: as many workers as
@@ -179,7 +191,8 @@ __device__ __forceinline__ Place find_place(PlaceScratch &at, int items, int cop
         });
     if (list && tid == 0) list[items] = one;
     __syncthreads();
-    p.before = at.before, p.item = (int)at.item;
+    p.total = uniform(p.total), p.start = uniform(p.start), p.stop = uniform(p.stop), p.copy = uniform(p.copy);
+    p.before = uniform(at.before), p.item = uniform((int)at.item);
     __syncthreads();
     return p;
 }
@@ -216,7 +229,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
     constexpr int kQ = sizeof(T) == 4 ? 3 : 1, kP = sizeof(T) == 4 ? 3 : 2;      // bf16 parts of a query's element and of a weight
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, col = lane & 15;
-    const int worker = blockIdx.x, group = a.q_heads / a.kv_heads, shift = a.t.page_shift, in_page = (1 << shift) - 1;
+    const int worker = blockIdx.x, group = uniform(a.q_heads / a.kv_heads), shift = a.t.page_shift, in_page = (1 << shift) - 1;
     const Place place = find_place(*reinterpret_cast<PlaceScratch *>(smem), a.t.sequences, 1, worker, gridDim.x,
                                    worker == 0 ? a.few_before : nullptr, [&](int i, int to, auto &&take) {
                                        for (; i < to; ++i) take(i, few_tiles(a, span(a, i)) * a.kv_heads);
@@ -234,18 +247,25 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
         off_k[i] = (row & 15) * D + ((at ^ turn_k<D>(row)) << 4);
         off_v[i] = (row & 15) * D + ((at ^ turn_v<D>(row)) << 4);
     }
+    // where it finds its operands in a stage
+    int at_k[2][D / 64], at_v[D / 16];
     const int v_row = (col >> 1 & 3) + 4 * g + (col >> 3) * 16;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) at_k[h][j] = (16 * h + col) * D + (((4 * j + g) ^ turn_k<D>(16 * h + col)) << 4);
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) at_v[d] = 32 * D + v_row * D + ((d ^ turn_v<D>(v_row)) << 4) + (col & 1) * 8;
     const float sign = a.scale > 0.f ? 1.f : a.scale < 0.f ? -1.f : 0.f, c = log2_scale(a);
 
-    int s = __builtin_amdgcn_readfirstlane(place.item);
-    Span r = span(a, s);
+    int s = place.item;
+    Span r = uniform(span(a, s));
     int tiles = few_tiles(a, r);
-    int head = (int)((x - place.before) / tiles), t0 = (int)((x - place.before) - (int64_t)head * tiles);
+    int head = uniform((int)((x - place.before) / tiles)), t0 = uniform((int)((x - place.before) - (int64_t)head * tiles));
     bool first = true;
     while (x < stop) {
-        const int n = (int)min((int64_t)(tiles - t0), stop - x), rows = r.q.count * group;
-        const int held = __builtin_amdgcn_readfirstlane(r.q.held), end = __builtin_amdgcn_readfirstlane(r.end);
-        const int from = __builtin_amdgcn_readfirstlane(r.begin) + t0 * kFewKeys + 32 * wave;  // this wave's first key
+        const int n = uniform((int)min((int64_t)(tiles - t0), stop - x)), rows = r.q.count * group;
+        const int held = r.q.held, end = r.end, from = r.begin + t0 * kFewKeys + 32 * wave;  // this wave's first key
 
         // this lane's query (columns without one repeat another)
         const int token = col / group, position = held + token, last = held + r.q.count - 1;
@@ -304,32 +324,41 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
         float m = -INFINITY, l = 0.f;
         Block ahead[kStages];
 #pragma unroll
-        for (int i = 0; i < kStages - 1; ++i) ahead[i] = issue(i);
+        for (int i = 0; i < kStages; ++i) ahead[i] = issue(i);
+        int stage = 0;
         for (int i = 0; i < n; ++i) {
-            wait_lds();  // the block before this one has been read
-            fence();
-            ahead[kStages - 1] = issue(i + kStages - 1);
             wait_vmem<(kStages - 1) * kLoads>();
+            fence();
+            // the block goes to registers at once, and the next one of its stage is on its way while it is computed
+            int4v_t raw_k[2][D / 64];
+            int2v_t raw_v[D / 16];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < D / 64; ++j) raw_k[h][j] = *reinterpret_cast<const int4v_t *>(ring + stage + at_k[h][j]);
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d)
+                raw_v[d] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) int2v_t *)(ring + stage + at_v[d]));
+            wait_lds();
             fence();
             const Block now = ahead[0];
 #pragma unroll
             for (int j = 0; j + 1 < kStages; ++j) ahead[j] = ahead[j + 1];
+            ahead[kStages - 1] = issue(i + kStages);
+            stage = stage + kStage == kStages * kStage ? 0 : stage + kStage;
             const int k = from + i * kFewKeys;
             if (k >= end) continue;
-            const char *const in_k = ring + (i % kStages) * kStage, *const in_v = in_k + 32 * D;
 
             float4_t sc[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const float power = scale_of(now.scales >> (16 * h) & 255);
-                const int row = 16 * h + col;
                 sc[h] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int j = 0; j < D / 64; ++j) {
-                    const int4v_t w = *reinterpret_cast<const int4v_t *>(in_k + row * D + (((4 * j + g) ^ turn_k<D>(row)) << 4));
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const bf16x8_t f = widen_eight(w[2 * e], w[2 * e + 1], power, power);
+                        const bf16x8_t f = widen_eight(raw_k[h][j][2 * e], raw_k[h][j][2 * e + 1], power, power);
 #pragma unroll
                         for (int p = kQ - 1; p >= 0; --p) sc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, q[2 * j + e][p], sc[h], 0, 0, 0);
                     }
@@ -369,9 +398,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
             const float power0 = scale_of(now.scales >> 8 & 255), power1 = scale_of(now.scales >> 24);
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) {
-                int2v_t v = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                    (__attribute__((address_space(3))) int2v_t *)(in_v + v_row * D + ((d ^ turn_v<D>(v_row)) << 4) + (col & 1) * 8));
-                const bf16x8_t f = widen_eight(v[0] & keep[0], v[1] & keep[1], power0, power1);
+                const bf16x8_t f = widen_eight(raw_v[d][0] & keep[0], raw_v[d][1] & keep[1], power0, power1);
 #pragma unroll
                 for (int e = kP - 1; e >= 0; --e) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, w[e], o[d], 0, 0, 0);
             }
@@ -419,7 +446,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
         x += n, t0 = 0;
         if (x < stop && ++head == a.kv_heads) {
             head = 0;
-            do r = span(a, ++s), tiles = few_tiles(a, r);
+            do r = uniform(span(a, ++s)), tiles = few_tiles(a, r);
             while (tiles == 0);
         }
     }
@@ -458,6 +485,7 @@ inline int64_t many_units(int64_t tokens, int64_t sequences, int64_t group) { re
 
 // The keys that a row tile needs: [begin, end), begin on a border of 64
 struct Keys { int begin, end, tiles; };
+__device__ __forceinline__ Keys uniform(Keys k) { return Keys{uniform(k.begin), uniform(k.end), uniform(k.tiles)}; }
 __device__ __forceinline__ Keys many_keys(const AttentionArgs &a, const Span &r, int tile)
 {
     const int group = a.q_heads / a.kv_heads, rows = r.q.count * group, row = tile * kManyRows;
@@ -477,7 +505,7 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
     constexpr int kQ = sizeof(T) == 4 ? 3 : 1, kP = sizeof(T) == 4 ? 3 : 1;     // bf16 parts of a query's element and of a weight
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, col = lane & 31;
-    const int group = a.q_heads / a.kv_heads, shift = a.t.page_shift, in_page = (1 << shift) - 1;
+    const int group = uniform(a.q_heads / a.kv_heads), shift = a.t.page_shift, in_page = (1 << shift) - 1;
     const int worker = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);  // (a multiple of 8 workgroups)
 
     // first tokens of the sequences, where they fit
@@ -512,21 +540,27 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
         off_k[i] = row * D + ((at ^ turn_k<D>(row + 16 * wave)) << 4);
         off_v[i] = row * D + ((at ^ turn_many_v<D>(row + 16 * wave)) << 4);
     }
+    // where it finds its operands in a stage: of the first 32 keys, and of the first 16
+    int at_k[D / 32], at_v[D / 32];
     const int v_row = 4 * g + (lane >> 1 & 3) + (lane >> 3 & 1) * 8;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
+        at_k[j] = col * D + (((2 * j + g) ^ turn_k<D>(col)) << 4);
+        at_v[j] = (kManyKeys + v_row) * D + (((2 * j + (lane >> 4 & 1)) ^ turn_many_v<D>(v_row)) << 4) + (lane & 1) * 8;
+    }
     const float sign = a.scale > 0.f ? 1.f : a.scale < 0.f ? -1.f : 0.f, c = log2_scale(a);
 
-    int head = __builtin_amdgcn_readfirstlane(place.copy), u = __builtin_amdgcn_readfirstlane(place.item);
+    int head = place.copy, u = place.item;
     int s = find_sequence(a.t.sequences, u, [&](int i) { return many_start(a, i); });
-    Span r = span(a, s);
-    int tile = u - many_start(a, s);
-    int t0 = (int)(x - head * (place.total / a.kv_heads) - place.before);
+    Span r = uniform(span(a, s));
+    int tile = u - uniform(many_start(a, s));
+    int t0 = uniform((int)(x - head * (place.total / a.kv_heads) - place.before));
     bool first = true;
     while (true) {
-        const Keys keys = many_keys(a, r, tile);
-        const int n = (int)min((int64_t)(keys.tiles - t0), stop - x), rows = r.q.count * group;
+        const Keys keys = uniform(many_keys(a, r, tile));
+        const int n = uniform((int)min((int64_t)(keys.tiles - t0), stop - x)), rows = r.q.count * group;
         if (n < 1) return;  // (only where cu does not ascend)
-        const int held = __builtin_amdgcn_readfirstlane(r.q.held), end = __builtin_amdgcn_readfirstlane(keys.end);
-        const int from = __builtin_amdgcn_readfirstlane(keys.begin) + t0 * kManyKeys;
+        const int held = r.q.held, end = keys.end, from = keys.begin + t0 * kManyKeys;
         const int row0 = tile * kManyRows + 32 * wave, row = row0 + col;  // this wave's first row, and this lane's
         const int token = min(row, rows - 1) / group, of_group = min(row, rows - 1) - token * group, position = held + token;
         // positions of the wave's first and last row, by which its blocks are taken, masked or left out
@@ -560,114 +594,135 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
             wait_vmem<0>();
             asm volatile("" : "+v"(page), "+v"(scales));
         };
-        struct Block { uint32_t scales[4]; };
+        struct Block { uint32_t scales0, scales1, scales2, scales3; };  // of its four pieces
+        int to_stage = 0, stage = 0;
         auto issue = [&](int i) {
             if ((i & 15) == 0) look_up(i);
             const int piece = 4 * (i & 15), p = __builtin_amdgcn_readlane(page, piece + wave);
             const rsrc_t in_k = block_rsrc(a.k_pages, a, p, head, D), in_v = block_rsrc(a.v_pages, a, p, head, D);
             const uint32_t at = (uint32_t)((from + i * kManyKeys + 16 * wave) & in_page) * D;
-            char *const to = smem + (i % kManyStages) * kStage + wave * 16 * D;
+            char *const to = smem + to_stage + wave * 16 * D;
+            to_stage = to_stage + kStage == kManyStages * kStage ? 0 : to_stage + kStage;
 #pragma unroll
             for (int j = 0; j < kLoads / 2; ++j) issue_load_to(in_k, off_k[j], at, to + j * 1024);
 #pragma unroll
             for (int j = 0; j < kLoads / 2; ++j) issue_load_to(in_v, off_v[j], at, to + kManyKeys * D + j * 1024);
-            Block b;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) b.scales[j] = (uint32_t)__builtin_amdgcn_readlane((int)scales, piece + j);
-            return b;
+            const auto of = [&](int j) { return (uint32_t)__builtin_amdgcn_readlane((int)scales, piece + j); };
+            return Block{of(0), of(1), of(2), of(3)};
         };
 
         float16_t o[D / 32];
 #pragma unroll
         for (int d = 0; d < D / 32; ++d) o[d] = float16_t{};
         float m = -INFINITY, l = 0.f;
-        Block ahead[kManyStages];
-        ahead[0] = issue(0);
-        ahead[1] = issue(1);
-        for (int i = 0; i < n; ++i) {
-            wait_vmem<kLoads>();  // this wave's part of the block has arrived, and what it read of the one before
-            wait_lds();
-            wg_barrier();
-            ahead[2] = issue(i + 2);
-            const Block now = ahead[0];
-            ahead[0] = ahead[1], ahead[1] = ahead[2];
-            const int k = from + i * kManyKeys;
-            if (!active || k > high || (a.window && k + kManyKeys - 1 <= low - a.window)) continue;
-            const char *const in_k = smem + (i % kManyStages) * kStage, *const in_v = in_k + kManyKeys * D;
-
-            float16_t sc[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float power = scale_of((col < 16 ? now.scales[2 * h] : now.scales[2 * h + 1]) & 255);
-                const int at = 32 * h + col;
-                sc[h] = float16_t{};
-#pragma unroll
-                for (int j = 0; j < D / 32; ++j) {
-                    const int4v_t w = *reinterpret_cast<const int4v_t *>(in_k + at * D + (((2 * j + g) ^ turn_k<D>(at)) << 4));
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const bf16x8_t f = widen_eight(w[2 * e], w[2 * e + 1], power, power);
-#pragma unroll
-                        for (int p = kQ - 1; p >= 0; --p) sc[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, q[2 * j + e][p], sc[h], 0, 0, 0);
+        // A maximum that rises by more than 2^8 leaves the loop, which takes the block up again behind it: sums that are scaled on
+        // one of two paths inside would be copied on the other, 64 registers for each block.
+        Block now = issue(0), next = issue(1), of = now;
+        const char *in = smem;
+        bool loaded = false, there = true;
+        int i = 0;
+        while (i < n) {
+            float raised = -INFINITY;
+            for (; i < n; ++i) {
+                const int k = from + i * kManyKeys;
+                if (!loaded) {
+                    wait_vmem<kLoads>();  // this wave's part of the block has arrived, and what it read of the one before
+                    wait_lds();
+                    wg_barrier();
+                    of = now, now = next, next = issue(i + 2);
+                    in = smem + stage;
+                    stage = stage + kStage == kManyStages * kStage ? 0 : stage + kStage;
+                    there = (of.scales0 & of.scales1 & of.scales2 & of.scales3) >> 16;
+                    if (!there || k + kManyKeys > end) {
+                        // values that are not there: zeros, whatever lies in their places (a weight of zero does not cancel a NaN)
+                        for (int j = tid; j < kManyKeys * D / 16; j += 256) {
+                            const int row = j / (D / 16);
+                            const uint32_t piece = row < 32 ? (row < 16 ? of.scales0 : of.scales1) : (row < 48 ? of.scales2 : of.scales3);
+                            if (!(piece >> 16) || k + row >= end)
+                                *reinterpret_cast<uint4_t *>(const_cast<char *>(in) + kManyKeys * D + 16 * j) = uint4_t{0, 0, 0, 0};
+                        }
+                        wait_lds();
+                        wg_barrier();
                     }
                 }
-            }
-            const bool all_there = (now.scales[0] & now.scales[1] & now.scales[2] & now.scales[3]) >> 16;
-            const bool edge = !all_there || k + kManyKeys - 1 > low || (a.window && k <= high - a.window);
-            if (edge) {
+                loaded = false;
+                if (!active || k > high || (a.window && k + kManyKeys - 1 <= low - a.window)) continue;
+
+                const uint32_t of_piece[4] = {of.scales0, of.scales1, of.scales2, of.scales3};
+                int4v_t raw_k[2][D / 32];
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int key = k + 32 * h + 8 * (e >> 2) + 4 * g + (e & 3);
-                        const bool seen = (now.scales[2 * h + (e >> 3)] >> 16) && key < end && key <= position && (!a.window || key > position - a.window);
-                        sc[h][e] = seen ? sc[h][e] : -INFINITY;
-                    }
-            }
-            float top = sc[0][0];
+                    for (int j = 0; j < D / 32; ++j) raw_k[h][j] = *reinterpret_cast<const int4v_t *>(in + at_k[j] + 32 * h * D);
+                float16_t sc[2];
 #pragma unroll
-            for (int e = 1; e < 32; ++e) top = __builtin_fmaxf(top, sc[e >> 4][e & 15]);
-            float t_a, t_b;
-            swap32(top, t_a, t_b);
-            top = __builtin_fmaxf(t_a, t_b);
-            if (__ballot((top - m) * c > 8.f)) {  // (false for two infinities of the same sign)
-                const float next = __builtin_fmaxf(m, top);
-                const float shrink = weight(m, c, next == -INFINITY ? 0.f : next * c);
-                l *= shrink;
+                for (int h = 0; h < 2; ++h) {
+                    const float power = col < 16 ? scale_of(of_piece[2 * h] & 255) : scale_of(of_piece[2 * h + 1] & 255);
+                    sc[h] = float16_t{};
 #pragma unroll
-                for (int d = 0; d < D / 32; ++d)
+                    for (int j = 0; j < D / 32; ++j)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) o[d][e] *= shrink;
-                m = next;
-            }
-            const float top_c = m == -INFINITY ? 0.f : m * c;
+                        for (int e = 0; e < 2; ++e) {
+                            const bf16x8_t f = widen_eight(raw_k[h][j][2 * e], raw_k[h][j][2 * e + 1], power, power);
 #pragma unroll
-            for (int step = 0; step < 4; ++step) {
-                float p[8];
+                            for (int p = kQ - 1; p >= 0; --p) sc[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, q[2 * j + e][p], sc[h], 0, 0, 0);
+                        }
+                }
+                int2v_t raw_v[4][D / 32];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) p[e] = weight(sc[step >> 1][8 * (step & 1) + e], c, top_c);
-                l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-                bf16x8_t w[kP];
-                split_eight(p, w);
-                const float power = scale_of(now.scales[step] >> 8 & 255);
-                int keep[2] = {-1, -1};  // bytes of V that are keys
-                if (edge) {
+                for (int step = 0; step < 4; ++step)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int left = (now.scales[step] >> 16) ? end - (k + 16 * step + 8 * h + 4 * g) : 0;
-                        keep[h] = left >= 4 ? -1 : left <= 0 ? 0 : (1 << (8 * left)) - 1;
+                    for (int d = 0; d < D / 32; ++d)
+                        raw_v[step][d] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) int2v_t *)(in + at_v[d] + 16 * step * D));
+                if (!there || k + kManyKeys - 1 > low || (a.window && k <= high - a.window)) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const int key = k + 32 * h + 8 * (e >> 2) + 4 * g + (e & 3);
+                            const bool seen = (of_piece[2 * h + (e >> 3)] >> 16) && key < end && key <= position && (!a.window || key > position - a.window);
+                            sc[h][e] = seen ? sc[h][e] : -INFINITY;
+                        }
+                }
+                float top = sc[0][0];
+#pragma unroll
+                for (int e = 1; e < 32; ++e) top = __builtin_fmaxf(top, sc[e >> 4][e & 15]);
+                float t_a, t_b;
+                swap32(top, t_a, t_b);
+                top = __builtin_fmaxf(t_a, t_b);
+                if (__ballot(m > -INFINITY && (top - m) * c > 8.f)) {
+                    raised = top;
+                    break;
+                }
+                m = m == -INFINITY ? top : m;  // (its sums are zeros so far)
+                const float top_c = m == -INFINITY ? 0.f : m * c;
+#pragma unroll
+                for (int step = 0; step < 4; ++step) {
+                    float p[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) p[e] = weight(sc[step >> 1][8 * (step & 1) + e], c, top_c);
+                    l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+                    bf16x8_t w[kP];
+                    split_eight(p, w);
+                    const float power = scale_of(of_piece[step] >> 8 & 255);
+#pragma unroll
+                    for (int d = 0; d < D / 32; ++d) {
+                        const bf16x8_t f = widen_eight(raw_v[step][d][0], raw_v[step][d][1], power, power);
+#pragma unroll
+                        for (int e = kP - 1; e >= 0; --e) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, w[e], o[d], 0, 0, 0);
                     }
                 }
-                const int at = 16 * step + v_row;
-#pragma unroll
-                for (int d = 0; d < D / 32; ++d) {
-                    const int2v_t v = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                        (__attribute__((address_space(3))) int2v_t *)(in_v + at * D + (((2 * d + (lane >> 4 & 1)) ^ turn_many_v<D>(at)) << 4) + (lane & 1) * 8));
-                    const bf16x8_t f = widen_eight(v[0] & keep[0], v[1] & keep[1], power, power);
-#pragma unroll
-                    for (int e = kP - 1; e >= 0; --e) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, w[e], o[d], 0, 0, 0);
-                }
             }
+            if (i == n) break;
+            loaded = true;
+            raised = __builtin_fmaxf(m, raised);
+            const float shrink = m == -INFINITY ? 1.f : weight(m, c, raised * c);
+            l *= shrink;
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[d][e] *= shrink;
+            m = raised;
         }
         wait_vmem_and_lds<0>();
         wg_barrier();  // the stages are free
@@ -700,11 +755,11 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
             if (++u == units) {
                 u = 0, s = 0;
                 if (++head == a.kv_heads) return;  // (only where cu does not ascend)
-                r = span(a, s);
+                r = uniform(span(a, s));
             }
-            while (s + 1 < a.t.sequences && many_start(a, s + 1) <= u) r = span(a, ++s);
-            tile = u - many_start(a, s);
-        } while (many_keys(a, r, tile).tiles == 0);
+            while (s + 1 < a.t.sequences && uniform(many_start(a, s + 1)) <= u) r = uniform(span(a, ++s));
+            tile = u - uniform(many_start(a, s));
+        } while (uniform(many_keys(a, r, tile)).tiles == 0);
     }
 }
 
