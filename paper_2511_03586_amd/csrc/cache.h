@@ -29,14 +29,11 @@ struct Sequence {
 
 __device__ __forceinline__ int first_token(const PageTable &t, int s) { return min(max(t.cu[s], 0), t.tokens); }
 
-__device__ __forceinline__ Sequence sequence(const PageTable &t, int s)
+__device__ __forceinline__ Sequence sequence(int first, int next, int length)
 {
-    Sequence q;
-    q.first = first_token(t, s);
-    q.held = min(t.lengths[s], (int)kMaxPosition);
-    q.count = q.held < 0 ? 0 : max(first_token(t, s + 1) - q.first, 0);
-    return q;
+    return Sequence{first, length < 0 ? 0 : max(next - first, 0), min(length, (int)kMaxPosition)};
 }
+__device__ __forceinline__ Sequence sequence(const PageTable &t, int s) { return sequence(first_token(t, s), first_token(t, s + 1), t.lengths[s]); }
 
 // Page of a sequence's column, or -1 where the table has none
 __device__ __forceinline__ int page_at(const PageTable &t, int s, int column)

@@ -17,9 +17,17 @@ struct AttentionArgs {
     int64_t ldq, ldo;
     int q_heads, kv_heads, max_tokens, window;
     float scale;
-    // scratch of the kernels for few and for many rows: tiles before each sequence or row tile, and the sums that workgroups leave
-    int64_t *few_before, *many_before;
+    // scratch of the kernels for few and for many rows: what is to be joined, and the sums that workgroups leave
+    struct Join *few_join, *many_join;
     float *few_partial, *many_partial;
+};
+
+// A tile of rows whose keys several workgroups have: the first of them left its sums in slot 2 from + odd, the others of `count`
+// in slots 2 (from + 1), 2 (from + 2), ...  Written by the second of them; count is 0 where a run cuts no tile or not first.
+struct Join {
+    int count, from, odd;
+    int first, row0, rows, head;  // the sequence's first token; the tile's first row, and its rows; head of the cache
+    int unused;
 };
 
 // Elements d .. d + 3 of a query and head from the sums of weights and of weighted values
@@ -125,15 +133,16 @@ struct Span {
     Sequence q;
     int begin, end;
 };
-__device__ __forceinline__ Span span(const AttentionArgs &a, int s)
+__device__ __forceinline__ Span span(const AttentionArgs &a, Sequence q)
 {
     Span r;
-    r.q = sequence(a.t, s);
+    r.q = q;
     r.q.count = min(r.q.count, a.max_tokens);
     r.end = (int)min((int64_t)r.q.held + r.q.count, (int64_t)a.t.columns << a.t.page_shift);
     r.begin = a.window ? max(r.q.held - a.window + 1, 0) & ~31 : 0;
     return r;
 }
+__device__ __forceinline__ Span span(const AttentionArgs &a, int s) { return span(a, sequence(a.t, s)); }
 __device__ __forceinline__ Span uniform(Span r)
 {
     return Span{Sequence{uniform(r.q.first), uniform(r.q.count), uniform(r.q.held)}, uniform(r.begin), uniform(r.end)};
@@ -145,8 +154,8 @@ __device__ __forceinline__ int workers_of(int64_t total, int workers) { return (
 __device__ __forceinline__ int64_t run_start(int64_t total, int worker, int workers) { return total * worker / workers; }
 __device__ __forceinline__ int worker_of(int64_t total, int64_t tile, int workers) { return (int)(((tile + 1) * workers - 1) / total); }
 
-// Tiles before each of `items` (each thread adds up a run of them) and of all, `copies` times over.  The item in which the run of
-// `worker` begins and the tiles before it are found on the way; `list` receives the tiles before all of them, [items + 1].
+// Tiles of each of `items` (each thread adds up a run of them) and of all, `copies` times over.  The item in which the run of
+// `worker` begins and the tiles before it are found on the way.
 struct Place {
     int64_t total, start, stop;  // tiles of all copies, and this worker's run of them
     int64_t before;              // of one copy, before the item
@@ -154,7 +163,7 @@ struct Place {
 };
 struct PlaceScratch { int64_t of_wave[4], before, item; };
 template <typename Tiles>
-__device__ __forceinline__ Place find_place(PlaceScratch &at, int items, int copies, int worker, int most, int64_t *list, Tiles &&tiles_of)
+__device__ __forceinline__ Place find_place(PlaceScratch &at, int items, int copies, int worker, int most, Tiles &&tiles_of)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int each = (items + 255) / 256, from = min(tid * each, items), to = min(from + each, items);
@@ -183,18 +192,27 @@ __device__ __forceinline__ Place find_place(PlaceScratch &at, int items, int cop
     p.copy = some ? (int)(p.start / one) : 0;
     const int64_t x = p.start - p.copy * one;
     int64_t before = upto - mine;
-    if (list || (some && x >= before && x < upto))
+    if (some && x >= before && x < upto)
         tiles_of(from, to, [&](int i, int n) {
-            if (list) list[i] = before;
             if (x >= before && x < before + n) at.before = before, at.item = i;
             before += n;
         });
-    if (list && tid == 0) list[items] = one;
     __syncthreads();
     p.total = uniform(p.total), p.start = uniform(p.start), p.stop = uniform(p.stop), p.copy = uniform(p.copy);
     p.before = uniform(at.before), p.item = uniform((int)at.item);
     __syncthreads();
     return p;
+}
+
+// What has to be joined where the run of `worker` begins, in a tile of rows whose `tiles` begin with `start`
+__device__ __forceinline__ Join join_at(const Place &p, int worker, int workers, int64_t start, int tiles, Join j)
+{
+    j.count = 0, j.from = worker - 1, j.odd = 0, j.unused = 0;
+    if (start < p.start && start >= run_start(p.total, worker - 1, workers)) {
+        j.count = worker_of(p.total, start + tiles - 1, workers) - j.from + 1;
+        j.odd = run_start(p.total, worker - 1, workers) < start;
+    }
+    return j;
 }
 
 // ---- few rows: up to 16 of (token, head of a group) ---------------------------------------------------------------------
@@ -230,13 +248,15 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, col = lane & 15;
     const int worker = blockIdx.x, group = uniform(a.q_heads / a.kv_heads), shift = a.t.page_shift, in_page = (1 << shift) - 1;
-    const Place place = find_place(*reinterpret_cast<PlaceScratch *>(smem), a.t.sequences, 1, worker, gridDim.x,
-                                   worker == 0 ? a.few_before : nullptr, [&](int i, int to, auto &&take) {
+    const Place place = find_place(*reinterpret_cast<PlaceScratch *>(smem), a.t.sequences, 1, worker, gridDim.x, [&](int i, int to, auto &&take) {
                                        for (; i < to; ++i) take(i, few_tiles(a, span(a, i)) * a.kv_heads);
                                    });
     int64_t x = place.start;
     const int64_t stop = place.stop;
-    if (x >= stop) return;
+    if (x >= stop) {
+        if (tid == 0) a.few_join[worker].count = 0;
+        return;
+    }
 
     char *const ring = smem + wave * kStages * kStage;
     // a lane's 16 bytes of load i: row of the block's half and chunk
@@ -262,6 +282,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
     Span r = uniform(span(a, s));
     int tiles = few_tiles(a, r);
     int head = uniform((int)((x - place.before) / tiles)), t0 = uniform((int)((x - place.before) - (int64_t)head * tiles));
+    if (tid == 0)
+        a.few_join[worker] = join_at(place, worker, workers_of(place.total, gridDim.x), x - t0, tiles, Join{0, 0, 0, r.q.first, 0, r.q.count * group, head, 0});
     bool first = true;
     while (x < stop) {
         const int n = uniform((int)min((int64_t)(tiles - t0), stop - x)), rows = r.q.count * group;
@@ -453,46 +475,45 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
 }
 
 // ---- many rows --------------------------------------------------------------------------------------------------------------
-// Prompts: bound by the matrix units and by the vector work beside them.  Tiles of 128 rows of (token, head of a group) and one
+// Prompts: bound by the matrix units and by the vector work beside them.  Tiles of 256 rows (128 for heads of 256) of (token, head of a group) and one
 // head of the cache meet its keys 64 at a time, which pass through three stages of LDS, loaded by all four waves, one barrier to a
-// block; each wave has 32 rows.  The blocks of all row tiles and heads are one list, cut into equal runs as above, heads first: an
+// block; each wave has 64 of the rows (32).  The blocks of all row tiles and heads are one list, cut into equal runs as above, heads first: an
 // XCD's workgroups take neighbouring runs, which share keys in its L2.
 //
 // The products are those above on v_mfma_f32_32x32x16_bf16: a lane has one query, and keys 4 g .. 4 g + 3 of every eight (g =
 // lane / 32).  The weights of bf16 queries are rounded to bf16 once (the few rows' kernel, which waits for memory, keeps 16 bits
 // of them): another product with what that leaves would cost half of the time again.  A running maximum is raised only by more
 // than 2^8 in weights, which fp32 sums carry as well: the sums are then seldom scaled.
-constexpr int kManyRows = 128, kManyKeys = 64, kManyStages = 3;
-
-template <int D> constexpr int many_lds() { return kManyStages * 2 * kManyKeys * D; }
+constexpr int kManyKeys = 64, kManyStages = 3;
+template <int D> constexpr int many_tiles() { return 1; }
+template <int D> constexpr int many_rows() { return 128 * many_tiles<D>(); }
 // workgroups to a CU: one where a wave needs more than 256 registers (its queries and sums)
 template <int D, typename T> constexpr int many_per_cu() { return D == 256 || (D == 128 && sizeof(T) == 4) ? 1 : 2; }
 template <int D, typename T> constexpr int many_workers() { return 256 * many_per_cu<D, T>(); }
-constexpr int kStartsInLds = 2048;
+constexpr int kSequencesInLds = 1024;
+template <int D> constexpr int many_lds() { return kManyStages * 2 * kManyKeys * D + (2 * kSequencesInLds + 1) * 4; }
 
 template <int D> __device__ __forceinline__ constexpr int turn_many_v(int r)
 {
     return D == 64 ? (((r >> 3) & 1) << 1) | ((r >> 2) & 1) : D == 128 ? (((r >> 1) & 1) << 1) | (((r >> 3) & 1) << 2) | ((r >> 2) & 1) : ((r & 3) << 1) | (((r >> 3) & 1) << 3) | ((r >> 2) & 1);
 }
 
-// Row tiles of a sequence begin at this number: those of `count` tokens are at most count * group / 128 + 1.
-// (Where cu does not ascend they overlap or leave gaps: then some rows are not computed, and nothing below relies on their order.)
-__device__ __forceinline__ int many_start(const AttentionArgs &a, int s)
-{
-    return s == 0 ? 0 : (int)((int64_t)first_token(a.t, s) * (a.q_heads / a.kv_heads) / kManyRows) + s;
-}
-inline int64_t many_units(int64_t tokens, int64_t sequences, int64_t group) { return tokens * group / kManyRows + sequences; }
+// Row tiles of a sequence, whose first new token is `first`, begin at this number: those of `count` tokens are at most
+// count * group / rows + 1.  (Where cu does not ascend they overlap or leave gaps: then some rows are not computed, and nothing
+// below relies on their order.)
+__device__ __forceinline__ int many_start(int first, int group, int rows, int s) { return s == 0 ? 0 : (int)((int64_t)first * group / rows) + s; }
+inline int64_t many_units(int64_t tokens, int64_t sequences, int64_t group, int rows) { return tokens * group / rows + sequences; }
 
 // The keys that a row tile needs: [begin, end), begin on a border of 64
 struct Keys { int begin, end, tiles; };
 __device__ __forceinline__ Keys uniform(Keys k) { return Keys{uniform(k.begin), uniform(k.end), uniform(k.tiles)}; }
-__device__ __forceinline__ Keys many_keys(const AttentionArgs &a, const Span &r, int tile)
+__device__ __forceinline__ Keys many_keys(const AttentionArgs &a, const Span &r, int group, int tile, int tile_rows)
 {
-    const int group = a.q_heads / a.kv_heads, rows = r.q.count * group, row = tile * kManyRows;
+    const int rows = r.q.count * group, row = tile * tile_rows;
     Keys k{0, 0, 0};
     if (row >= rows || is_few(a, r.q.count)) return k;
-    const int token0 = row / group, token1 = min(row + kManyRows, rows) - 1;
-    k.end = (int)min((int64_t)r.q.held + token1 / group + 1, (int64_t)a.t.columns << a.t.page_shift);
+    const int token0 = row / group, token1 = (min(row + tile_rows, rows) - 1) / group;
+    k.end = (int)min((int64_t)r.q.held + token1 + 1, (int64_t)a.t.columns << a.t.page_shift);
     k.begin = a.window ? max(r.q.held + token0 - a.window + 1, 0) & ~(kManyKeys - 1) : 0;
     k.tiles = max((k.end - k.begin + kManyKeys - 1) / kManyKeys, 1);
     return k;
@@ -503,34 +524,44 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
 {
     constexpr int kStage = 2 * kManyKeys * D, kLoads = D / 32;                  // loads of a wave and block: K, then V
     constexpr int kQ = sizeof(T) == 4 ? 3 : 1, kP = sizeof(T) == 4 ? 3 : 1;     // bf16 parts of a query's element and of a weight
+    constexpr int kTiles = many_tiles<D>(), kRows = many_rows<D>();
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, col = lane & 31;
-    const int group = uniform(a.q_heads / a.kv_heads), shift = a.t.page_shift, in_page = (1 << shift) - 1;
+    const int group = uniform(a.q_heads / a.kv_heads), shift = a.t.page_shift, in_page = (1 << shift) - 1, sequences = a.t.sequences;
     const int worker = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);  // (a multiple of 8 workgroups)
 
-    // first tokens of the sequences, where they fit
-    int *const starts = reinterpret_cast<int *>(smem + sizeof(PlaceScratch));
-    const bool in_lds = a.t.sequences <= kStartsInLds;
+    // the sequences' first tokens and lengths, where they fit
+    int *const firsts = reinterpret_cast<int *>(smem + kManyStages * kStage), *const lengths = firsts + kSequencesInLds + 1;
+    const bool in_lds = sequences <= kSequencesInLds;
     if (in_lds) {
-        for (int i = tid; i < a.t.sequences; i += 256) starts[i] = many_start(a, i);
+        for (int i = tid; i <= sequences; i += 256) firsts[i] = first_token(a.t, i);
+        for (int i = tid; i < sequences; i += 256) lengths[i] = a.t.lengths[i];
         __syncthreads();
     }
-    const auto start_of = [&](int s) { return in_lds ? starts[s] : many_start(a, s); };
-    const Place place = find_place(*reinterpret_cast<PlaceScratch *>(smem), units, a.kv_heads, worker, gridDim.x, worker == 0 ? a.many_before : nullptr,
+    const auto first_of = [&](int s) { return in_lds ? firsts[s] : first_token(a.t, s); };
+    const auto start_of = [&](int s) { return many_start(first_of(s), group, kRows, s); };
+    const auto span_of = [&](int s) {
+        return in_lds ? span(a, sequence(firsts[s], firsts[s + 1], lengths[s])) : span(a, s);
+    };
+    const Place place = find_place(*reinterpret_cast<PlaceScratch *>(smem), units, a.kv_heads, worker, gridDim.x,
                                    [&](int u, int to, auto &&take) {
+                                       if (u >= to) return;
                                        int s = 0;  // the last sequence that begins at u or before
-                                       for (int n = a.t.sequences; n > 1;) {
+                                       for (int n = sequences; n > 1;) {
                                            const int half = n >> 1;
                                            if (start_of(s + half) <= u) s += half, n -= half; else n = half;
                                        }
                                        for (; u < to; ++u) {
-                                           while (s + 1 < a.t.sequences && start_of(s + 1) <= u) ++s;
-                                           take(u, many_keys(a, span(a, s), u - start_of(s)).tiles);
+                                           while (s + 1 < sequences && start_of(s + 1) <= u) ++s;
+                                           take(u, many_keys(a, span_of(s), group, u - start_of(s), kRows).tiles);
                                        }
                                    });
     int64_t x = place.start;
     const int64_t stop = place.stop;
-    if (x >= stop) return;
+    if (x >= stop) {
+        if (tid == 0) a.many_join[worker].count = 0;
+        return;
+    }
 
     // a lane's 16 bytes of load i of its wave's 16 rows
     uint32_t off_k[kLoads / 2], off_v[kLoads / 2];
@@ -551,25 +582,44 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
     const float sign = a.scale > 0.f ? 1.f : a.scale < 0.f ? -1.f : 0.f, c = log2_scale(a);
 
     int head = place.copy, u = place.item;
-    int s = find_sequence(a.t.sequences, u, [&](int i) { return many_start(a, i); });
-    Span r = uniform(span(a, s));
-    int tile = u - uniform(many_start(a, s));
+    int s = find_sequence(sequences, u, start_of);
+    Span r = uniform(span_of(s));
+    int tile = u - uniform(start_of(s));
     int t0 = uniform((int)(x - head * (place.total / a.kv_heads) - place.before));
+    if (tid == 0)
+        a.many_join[worker] = join_at(place, worker, workers_of(place.total, gridDim.x), x - t0, many_keys(a, r, group, tile, kRows).tiles,
+                                      Join{0, 0, 0, r.q.first, tile * kRows, min(r.q.count * group - tile * kRows, kRows), head, 0});
     bool first = true;
     while (true) {
-        const Keys keys = uniform(many_keys(a, r, tile));
+        const Keys keys = uniform(many_keys(a, r, group, tile, kRows));
         const int n = uniform((int)min((int64_t)(keys.tiles - t0), stop - x)), rows = r.q.count * group;
         if (n < 1) return;  // (only where cu does not ascend)
         const int held = r.q.held, end = keys.end, from = keys.begin + t0 * kManyKeys;
-        const int row0 = tile * kManyRows + 32 * wave, row = row0 + col;  // this wave's first row, and this lane's
-        const int token = min(row, rows - 1) / group, of_group = min(row, rows - 1) - token * group, position = held + token;
-        // positions of the wave's first and last row, by which its blocks are taken, masked or left out
-        const int low = __builtin_amdgcn_readfirstlane(position), high = __builtin_amdgcn_readlane(position, 31);
+        const int row0 = tile * kRows + 32 * kTiles * wave;  // this wave's first row
         const bool active = row0 < rows;
 
-        bf16x8_t q[D / 16][kQ];
-        {
-            const T *in = reinterpret_cast<const T *>(a.q) + (int64_t)(r.q.first + token) * a.ldq + (int64_t)(head * group + of_group) * D;
+        // Pages and scales of 64 pieces of 16 keys, one a lane: 16 blocks
+        int page = -1;
+        uint32_t scales = 0;  // bytes of K and V; bit 16: the page is there
+        const auto look_up_page = [&](int i) {
+            const int k = from + i * kManyKeys + 16 * lane;
+            page = k < end ? page_at(a.t, s, k >> shift) : -1;
+        };
+        const auto look_up_scales = [&] {
+            uint32_t b0 = 0, b1 = 0;
+            if (page >= 0) b0 = a.k_scales[(int64_t)page * a.kv_heads + head], b1 = a.v_scales[(int64_t)page * a.kv_heads + head];
+            scales = b0 | b1 << 8 | (page >= 0 ? 0x10000 : 0);
+        };
+        look_up_page(0);
+
+        // this lane's queries: rows, tokens, heads of the group
+        int position[kTiles], token[kTiles], of_group[kTiles];
+        bf16x8_t q[kTiles][D / 16][kQ];
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            const int row = min(row0 + 32 * t + col, rows - 1);
+            token[t] = row / group, of_group[t] = row - token[t] * group, position[t] = held + token[t];
+            const T *in = reinterpret_cast<const T *>(a.q) + (int64_t)(r.q.first + token[t]) * a.ldq + (int64_t)(head * group + of_group[t]) * D;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {
                 Eight<T> raw;
@@ -578,26 +628,24 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
                 raw.get(v);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] *= sign;
-                split_eight(v, q[i]);
+                split_eight(v, q[t][i]);
             }
         }
+        // positions of the wave's first and last row, by which its blocks are taken, masked or left out
+        const int low = __builtin_amdgcn_readfirstlane(position[0]), high = __builtin_amdgcn_readlane(position[kTiles - 1], 31);
+        look_up_scales();
+        wait_vmem<0>();
+        asm volatile("" : "+v"(page), "+v"(scales));
 
-        // Pages and scales of 64 pieces of 16 keys, one a lane: 16 blocks
-        int page = -1;
-        uint32_t scales = 0;  // bytes of K and V; bit 16: the page is there
-        auto look_up = [&](int i) {
-            const int k = from + i * kManyKeys + 16 * lane;
-            page = k < end ? page_at(a.t, s, k >> shift) : -1;
-            uint32_t b0 = 0, b1 = 0;
-            if (page >= 0) b0 = a.k_scales[(int64_t)page * a.kv_heads + head], b1 = a.v_scales[(int64_t)page * a.kv_heads + head];
-            scales = b0 | b1 << 8 | (page >= 0 ? 0x10000 : 0);
-            wait_vmem<0>();
-            asm volatile("" : "+v"(page), "+v"(scales));
-        };
         struct Block { uint32_t scales0, scales1, scales2, scales3; };  // of its four pieces
         int to_stage = 0, stage = 0;
         auto issue = [&](int i) {
-            if ((i & 15) == 0) look_up(i);
+            if ((i & 15) == 0 && i) {
+                look_up_page(i);
+                look_up_scales();
+                wait_vmem<0>();
+                asm volatile("" : "+v"(page), "+v"(scales));
+            }
             const int piece = 4 * (i & 15), p = __builtin_amdgcn_readlane(page, piece + wave);
             const rsrc_t in_k = block_rsrc(a.k_pages, a, p, head, D), in_v = block_rsrc(a.v_pages, a, p, head, D);
             const uint32_t at = (uint32_t)((from + i * kManyKeys + 16 * wave) & in_page) * D;
@@ -611,18 +659,22 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
             return Block{of(0), of(1), of(2), of(3)};
         };
 
-        float16_t o[D / 32];
+        float16_t o[kTiles][D / 32];
+        float m[kTiles], l[kTiles];
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d) o[d] = float16_t{};
-        float m = -INFINITY, l = 0.f;
+        for (int t = 0; t < kTiles; ++t) {
+            m[t] = -INFINITY, l[t] = 0.f;
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d) o[t][d] = float16_t{};
+        }
         // A maximum that rises by more than 2^8 leaves the loop, which takes the block up again behind it: sums that are scaled on
-        // one of two paths inside would be copied on the other, 64 registers for each block.
+        // one of two paths inside would be copied on the other, all of them for each block.
         Block now = issue(0), next = issue(1), of = now;
         const char *in = smem;
         bool loaded = false, there = true;
         int i = 0;
         while (i < n) {
-            float raised = -INFINITY;
+            float raised[kTiles];
             for (; i < n; ++i) {
                 const int k = from + i * kManyKeys;
                 if (!loaded) {
@@ -654,98 +706,120 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int j = 0; j < D / 32; ++j) raw_k[h][j] = *reinterpret_cast<const int4v_t *>(in + at_k[j] + 32 * h * D);
-                float16_t sc[2];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float power = col < 16 ? scale_of(of_piece[2 * h] & 255) : scale_of(of_piece[2 * h + 1] & 255);
-                    sc[h] = float16_t{};
-#pragma unroll
-                    for (int j = 0; j < D / 32; ++j)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const bf16x8_t f = widen_eight(raw_k[h][j][2 * e], raw_k[h][j][2 * e + 1], power, power);
-#pragma unroll
-                            for (int p = kQ - 1; p >= 0; --p) sc[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, q[2 * j + e][p], sc[h], 0, 0, 0);
-                        }
-                }
                 int2v_t raw_v[4][D / 32];
 #pragma unroll
                 for (int step = 0; step < 4; ++step)
 #pragma unroll
                     for (int d = 0; d < D / 32; ++d)
                         raw_v[step][d] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) int2v_t *)(in + at_v[d] + 16 * step * D));
-                if (!there || k + kManyKeys - 1 > low || (a.window && k <= high - a.window)) {
+                float16_t sc[kTiles][2];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < 2; ++h) {
+                    const float power = col < 16 ? scale_of(of_piece[2 * h] & 255) : scale_of(of_piece[2 * h + 1] & 255);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const int key = k + 32 * h + 8 * (e >> 2) + 4 * g + (e & 3);
-                            const bool seen = (of_piece[2 * h + (e >> 3)] >> 16) && key < end && key <= position && (!a.window || key > position - a.window);
-                            sc[h][e] = seen ? sc[h][e] : -INFINITY;
+                    for (int t = 0; t < kTiles; ++t) sc[t][h] = float16_t{};
+#pragma unroll
+                    for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const bf16x8_t f = widen_eight(raw_k[h][j][2 * e], raw_k[h][j][2 * e + 1], power, power);
+#pragma unroll
+                            for (int p = kQ - 1; p >= 0; --p)
+#pragma unroll
+                                for (int t = 0; t < kTiles; ++t) sc[t][h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, q[t][2 * j + e][p], sc[t][h], 0, 0, 0);
                         }
                 }
-                float top = sc[0][0];
+                if (!there || k + kManyKeys - 1 > low || (a.window && k <= high - a.window)) {
 #pragma unroll
-                for (int e = 1; e < 32; ++e) top = __builtin_fmaxf(top, sc[e >> 4][e & 15]);
-                float t_a, t_b;
-                swap32(top, t_a, t_b);
-                top = __builtin_fmaxf(t_a, t_b);
-                if (__ballot(m > -INFINITY && (top - m) * c > 8.f)) {
-                    raised = top;
-                    break;
+                    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                const int key = k + 32 * h + 8 * (e >> 2) + 4 * g + (e & 3);
+                                const bool seen = (of_piece[2 * h + (e >> 3)] >> 16) && key < end && key <= position[t] && (!a.window || key > position[t] - a.window);
+                                sc[t][h][e] = seen ? sc[t][h][e] : -INFINITY;
+                            }
                 }
-                m = m == -INFINITY ? top : m;  // (its sums are zeros so far)
-                const float top_c = m == -INFINITY ? 0.f : m * c;
+                bool rises = false;
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                    float top = sc[t][0][0];
+#pragma unroll
+                    for (int e = 1; e < 32; ++e) top = __builtin_fmaxf(top, sc[t][e >> 4][e & 15]);
+                    float t_a, t_b;
+                    swap32(top, t_a, t_b);
+                    raised[t] = __builtin_fmaxf(t_a, t_b);
+                    rises |= m[t] > -INFINITY && (raised[t] - m[t]) * c > 8.f;
+                }
+                if (__ballot(rises)) break;
+                float top_c[kTiles];
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                    m[t] = m[t] == -INFINITY ? raised[t] : m[t];  // (its sums are zeros so far)
+                    top_c[t] = m[t] == -INFINITY ? 0.f : m[t] * c;
+                }
 #pragma unroll
                 for (int step = 0; step < 4; ++step) {
-                    float p[8];
+                    bf16x8_t w[kTiles][kP];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) p[e] = weight(sc[step >> 1][8 * (step & 1) + e], c, top_c);
-                    l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-                    bf16x8_t w[kP];
-                    split_eight(p, w);
+                    for (int t = 0; t < kTiles; ++t) {
+                        float p[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) p[e] = weight(sc[t][step >> 1][8 * (step & 1) + e], c, top_c[t]);
+                        l[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+                        split_eight(p, w[t]);
+                    }
                     const float power = scale_of(of_piece[step] >> 8 & 255);
 #pragma unroll
                     for (int d = 0; d < D / 32; ++d) {
                         const bf16x8_t f = widen_eight(raw_v[step][d][0], raw_v[step][d][1], power, power);
 #pragma unroll
-                        for (int e = kP - 1; e >= 0; --e) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, w[e], o[d], 0, 0, 0);
+                        for (int e = kP - 1; e >= 0; --e)
+#pragma unroll
+                            for (int t = 0; t < kTiles; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, w[t][e], o[t][d], 0, 0, 0);
                     }
                 }
             }
             if (i == n) break;
             loaded = true;
-            raised = __builtin_fmaxf(m, raised);
-            const float shrink = m == -INFINITY ? 1.f : weight(m, c, raised * c);
-            l *= shrink;
 #pragma unroll
-            for (int d = 0; d < D / 32; ++d)
+            for (int t = 0; t < kTiles; ++t) {
+                raised[t] = __builtin_fmaxf(m[t], raised[t]);
+                const float shrink = m[t] == -INFINITY ? 1.f : weight(m[t], c, raised[t] * c);
+                l[t] *= shrink;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[d][e] *= shrink;
-            m = raised;
+                for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[t][d][e] *= shrink;
+                m[t] = raised[t];
+            }
         }
         wait_vmem_and_lds<0>();
         wg_barrier();  // the stages are free
 
-        float l_a, l_b;
-        swap32(l, l_a, l_b);
-        l = l_a + l_b;
         const bool whole = n == keys.tiles;
-        if (row < rows) {
-            float *const out = whole ? nullptr : a.many_partial + (int64_t)(2 * worker + !first) * partial_floats(kManyRows, D);
-            const int in_tile = 32 * wave + col;
+        float *const out = whole ? nullptr : a.many_partial + (int64_t)(2 * worker + !first) * partial_floats(kRows, D);
 #pragma unroll
-            for (int d = 0; d < D / 32; ++d)
+        for (int t = 0; t < kTiles; ++t) {
+            float l_a, l_b;
+            swap32(l[t], l_a, l_b);
+            const float sum = l_a + l_b;
+            const int in_tile = 32 * (kTiles * wave + t) + col;
+            if (row0 + 32 * t + col < rows) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float4_t v = {o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]};
-                    const int at = 32 * d + 8 * e + 4 * g;
-                    if (whole)
-                        finish<T>(a, r.q.first + token, head * group + of_group, at, D, v, m, l);
-                    else
-                        *reinterpret_cast<float4_t *>(out + in_tile * D + at) = v;
-                }
-            if (!whole && g == 0) out[kManyRows * D + in_tile] = m, out[kManyRows * (D + 1) + in_tile] = l;
+                for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float4_t v = {o[t][d][4 * e], o[t][d][4 * e + 1], o[t][d][4 * e + 2], o[t][d][4 * e + 3]};
+                        const int at = 32 * d + 8 * e + 4 * g;
+                        if (whole)
+                            finish<T>(a, r.q.first + token[t], head * group + of_group[t], at, D, v, m[t], sum);
+                        else
+                            *reinterpret_cast<float4_t *>(out + in_tile * D + at) = v;
+                    }
+                if (!whole && g == 0) out[kRows * D + in_tile] = m[t], out[kRows * (D + 1) + in_tile] = sum;
+            }
         }
         first = false;
         x += n, t0 = 0;
@@ -755,56 +829,36 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
             if (++u == units) {
                 u = 0, s = 0;
                 if (++head == a.kv_heads) return;  // (only where cu does not ascend)
-                r = uniform(span(a, s));
+                r = uniform(span_of(s));
             }
-            while (s + 1 < a.t.sequences && uniform(many_start(a, s + 1)) <= u) r = uniform(span(a, ++s));
-            tile = u - uniform(many_start(a, s));
-        } while (uniform(many_keys(a, r, tile)).tiles == 0);
+            while (s + 1 < sequences && uniform(start_of(s + 1)) <= u) r = uniform(span_of(++s));
+            tile = u - uniform(start_of(s));
+        } while (uniform(many_keys(a, r, group, tile, kRows)).tiles == 0);
     }
 }
 
 // ---- both ----------------------------------------------------------------------------------------------------------------------
-// Joins what several workgroups have left of one tile of rows, in their order, the largest maximum first.  Only a tile that the
-// beginning of a run cuts was divided: a workgroup for each such beginning (the first in its tile) and kRows rows.  What few
-// workgroups left is added by the threads of a row; of more, all teams of D / 4 lanes take a share.
+// Joins what several workgroups have left of one tile of rows, in their order, the largest maximum first: a workgroup for each
+// beginning of a run and kRows rows.  What few workgroups left is added by the threads of a row; of more, all teams of D / 4
+// lanes take a share.
 template <int D, typename T, bool MANY>
-__global__ __launch_bounds__(256) void cache_attention_join_kernel(const AttentionArgs a, int units)
+__global__ __launch_bounds__(256) void cache_attention_join_kernel(const AttentionArgs a)
 {
-    constexpr int kRows = MANY ? 8 : 1, kTile = MANY ? kManyRows : kFewRows, kWorkers = MANY ? many_workers<D, T>() : few_workers<D>();
+    constexpr int kRows = MANY ? 8 : 1, kTile = MANY ? many_rows<D>() : kFewRows, kWorkers = MANY ? many_workers<D, T>() : few_workers<D>();
     constexpr int kLanes = D / 4, kTeams = 256 / kLanes, kSerial = 8;
     __shared__ float factor[kWorkers], of_wave[2][4];
     __shared__ float4_t sums[kTeams][kLanes];
-    const int tid = threadIdx.x, worker = blockIdx.x, group = a.q_heads / a.kv_heads, items = MANY ? units : a.t.sequences;
-    const int64_t *const before = MANY ? a.many_before : a.few_before;
+    const int tid = threadIdx.x, group = a.q_heads / a.kv_heads;
+    const Join j = (MANY ? a.many_join : a.few_join)[blockIdx.x];
+    const int count = j.count, rows = j.rows;
+    if (count == 0) return;
     const float *const partials = MANY ? a.many_partial : a.few_partial;
-    const int64_t one = before[items], total = MANY ? one * a.kv_heads : one;
-    const int workers = workers_of(total, kWorkers);
-    if (worker == 0 || worker >= workers) return;
-    const int64_t x = run_start(total, worker, workers), copy = MANY ? x / one : 0, in_copy = x - copy * one;
-    const int item = find_sequence(items, 0, [&](int i) { return before[i] <= in_copy ? 0 : 1; });
-    int s = item, tile = 0, head, tiles;
-    int64_t start;
-    Span r;
-    if constexpr (MANY) {
-        s = find_sequence(a.t.sequences, item, [&](int i) { return many_start(a, i); });
-        r = span(a, s), tile = item - many_start(a, s), head = (int)copy, start = copy * one + before[item];
-        tiles = many_keys(a, r, tile).tiles;
-    } else {
-        r = span(a, s);
-        tiles = few_tiles(a, r);
-        head = (int)((x - before[item]) / max(tiles, 1)), start = before[item] + (int64_t)head * tiles;
-    }
-    if (start >= x || start < run_start(total, worker - 1, workers) || start + tiles > total) return;
-    const int from = worker - 1, count = worker_of(total, start + tiles - 1, workers) - from + 1;
-    const int rows = min(r.q.count * group - tile * kTile, kTile);
-    const auto partial = [&](int i) {
-        return partials + (int64_t)(2 * (from + i) + (i == 0 && run_start(total, from, workers) < start)) * partial_floats(kTile, D);
-    };
+    const auto partial = [&](int i) { return partials + (int64_t)(2 * (j.from + i) + (i == 0 ? j.odd : 0)) * partial_floats(kTile, D); };
     const float c = log2_scale(a);
     const int d = tid % kLanes, team = tid / kLanes;
     const auto put = [&](int row, float4_t v, float top, float sum) {
-        const int of_all = tile * kTile + row, token = of_all / group;
-        finish<T>(a, r.q.first + token, head * group + of_all - token * group, 4 * d, D, v, top, sum);
+        const int of_all = j.row0 + row, token = of_all / group;
+        finish<T>(a, j.first + token, j.head * group + of_all - token * group, 4 * d, D, v, top, sum);
     };
     if (count <= kSerial) {
         for (int row = blockIdx.y * kRows + team; row < min((int)(blockIdx.y + 1) * kRows, rows); row += kTeams) {
@@ -862,36 +916,37 @@ __global__ __launch_bounds__(256) void cache_attention_join_kernel(const Attenti
     }
 }
 
-// Scratch: tiles before each sequence and row tile, then the sums
-struct Scratch { int64_t many_before, few_partial, many_partial, bytes; };  // where these begin, in bytes
-template <int D, typename T>
-static Scratch scratch(int64_t tokens, int64_t sequences, int64_t max_tokens, int64_t group)
+// Scratch: what is to be joined, then the sums
+struct Scratch { int64_t many_join, few_partial, many_partial, bytes; };  // where these begin, in bytes
+template <int D>
+static Scratch scratch(int64_t tokens, int64_t max_tokens, int64_t group)
 {
     const bool many = std::min(max_tokens, tokens) * group > kFewRows;
+    constexpr int kMany = many_workers<D, uint16_t>();  // (as many as of any type)
     Scratch s;
-    s.many_before = 8 * (sequences + 1);
-    s.few_partial = (s.many_before + (many ? 8 * (many_units(tokens, sequences, group) + 1) : 0) + 15) / 16 * 16;
+    s.many_join = few_workers<D>() * sizeof(Join);
+    s.few_partial = s.many_join + kMany * sizeof(Join);
     s.many_partial = s.few_partial + 8ll * few_workers<D>() * partial_floats(kFewRows, D);
-    s.bytes = s.many_partial + (many ? 8ll * many_workers<D, T>() * partial_floats(kManyRows, D) : 0);
+    s.bytes = s.many_partial + (many ? 8ll * kMany * partial_floats(many_rows<D>(), D) : 0);
     return s;
 }
 
 template <int D, typename T>
 static perf_status attention(AttentionArgs &a, char *workspace, hipStream_t st)
 {
-    const int64_t group = a.q_heads / a.kv_heads, units = many_units(a.t.tokens, a.t.sequences, group);
+    const int64_t group = a.q_heads / a.kv_heads, units = many_units(a.t.tokens, a.t.sequences, group, many_rows<D>());
     if (units > INT32_MAX) return PERF_ERR_UNSUPPORTED;
-    const Scratch at = scratch<D, T>(a.t.tokens, a.t.sequences, a.max_tokens, group);
-    a.few_before = (int64_t *)workspace, a.many_before = (int64_t *)(workspace + at.many_before);
+    const Scratch at = scratch<D>(a.t.tokens, a.max_tokens, group);
+    a.few_join = (Join *)workspace, a.many_join = (Join *)(workspace + at.many_join);
     a.few_partial = (float *)(workspace + at.few_partial), a.many_partial = (float *)(workspace + at.many_partial);
     const bool many = a.max_tokens * group > kFewRows;  // (whether a sequence of as many tokens is for the other kernel)
     if (!allow_lds<cache_attention_few_kernel<D, T>>(few_lds<D>())) return PERF_ERR_LAUNCH;
     cache_attention_few_kernel<D, T><<<few_workers<D>(), 256, few_lds<D>(), st>>>(a);
-    cache_attention_join_kernel<D, T, false><<<dim3(few_workers<D>(), (uint32_t)std::min<int64_t>(kFewRows, a.max_tokens * group)), 256, 0, st>>>(a, (int)units);
+    cache_attention_join_kernel<D, T, false><<<dim3(few_workers<D>(), (uint32_t)std::min<int64_t>(kFewRows, a.max_tokens * group)), 256, 0, st>>>(a);
     if (many) {
         if (!allow_lds<cache_attention_many_kernel<D, T>>(many_lds<D>())) return PERF_ERR_LAUNCH;
         cache_attention_many_kernel<D, T><<<many_workers<D, T>(), 256, many_lds<D>(), st>>>(a, (int)units);
-        cache_attention_join_kernel<D, T, true><<<dim3(many_workers<D, T>(), kManyRows / 8), 256, 0, st>>>(a, (int)units);
+        cache_attention_join_kernel<D, T, true><<<dim3(many_workers<D, T>(), many_rows<D>() / 8), 256, 0, st>>>(a);
     }
     return launch_status();
 }
@@ -911,10 +966,9 @@ extern "C" int64_t perf_cache_attention_fp8_workspace_bytes(int64_t tokens, int6
     const CacheShape c{tokens, sequences, q_heads, kv_heads, head_dim, 1, page_size, table_pages, table_pages};
     if (!attention_shape_ok(c, max_tokens) || !cache_supported(c)) return -1;
     const int64_t group = q_heads / kv_heads;
-    // (bf16 queries: no type needs more)
-    return (head_dim == 64    ? scratch<64, uint16_t>(tokens, sequences, max_tokens, group)
-            : head_dim == 128 ? scratch<128, uint16_t>(tokens, sequences, max_tokens, group)
-                              : scratch<256, uint16_t>(tokens, sequences, max_tokens, group))
+    return (head_dim == 64    ? scratch<64>(tokens, max_tokens, group)
+            : head_dim == 128 ? scratch<128>(tokens, max_tokens, group)
+                              : scratch<256>(tokens, max_tokens, group))
         .bytes;
 }
 
