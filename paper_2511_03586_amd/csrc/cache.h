@@ -43,19 +43,30 @@ __device__ __forceinline__ int page_at(const PageTable &t, int s, int column)
     return (uint32_t)p < (uint32_t)t.pages ? p : -1;
 }
 
-// The last sequence whose start(s) is at most `u`, where start ascends from at most u: the wave looks at 64 at a time.
+// The last sequence whose start(s) is at most `u`, where start ascends from at most u: a lane looks at up to four at a time, so
+// that 256 sequences cost one trip to memory.
 template <typename Start>
 __device__ __forceinline__ int find_sequence(int sequences, int u, Start &&start)
 {
+    constexpr int kEach = 4;
     const int lane = threadIdx.x & (kWave - 1);
     int from = 0, n = sequences;
     while (n > 1) {
-        const int step = (n + kWave - 1) / kWave;
-        const bool at_most = lane * step < n && start(from + lane * step) <= u;
-        const uint64_t b = __ballot(at_most);
-        const int i = b ? 63 - __builtin_clzll(b) : 0;
-        from += i * step;
-        n = min(step, n - i * step);
+        const int step = n <= kWave * kEach ? 1 : (n + kWave * kEach - 1) / (kWave * kEach);
+        int last = 0;
+        bool at_most[kEach];
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const int i = (j * kWave + lane) * step;
+            at_most[j] = i < n && start(from + i) <= u;
+        }
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const uint64_t b = __ballot(at_most[j]);
+            if (b) last = (j * kWave + 63 - __builtin_clzll(b)) * step;
+        }
+        from += last;
+        n = min(step, n - last);
     }
     return __builtin_amdgcn_readfirstlane(from);
 }

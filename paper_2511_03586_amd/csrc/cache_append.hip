@@ -6,8 +6,8 @@
 // contracts.  A scale is a power of two: what a page holds is moved to a larger one exactly but for subnormals, so that a page
 // that is filled token by token does not drift, and its values are exact in bf16.
 //
-// One launch: workgroups of (page that new tokens reach, head, keys or values), whose tokens stay in registers between the
-// maximum and the rounding, and waves of (token, eight heads' worth of a query row) behind them.
+// One launch: teams of waves for each (page that new tokens reach, head, keys or values), whose tokens stay in registers between
+// the maximum and the rounding, and waves of (token, part of a query row) behind them.
 #include "cache.h"
 #include "fp8.h"
 
@@ -21,7 +21,7 @@ struct AppendArgs {
     uint8_t *k_pages, *v_pages, *k_scales, *v_scales;
     int64_t ldq, ldk, ldv, ldq_out;
     int q_heads, kv_heads, rotary, positions, q_waves;
-    bool interleaved;
+    bool interleaved, by_token;
     uint32_t append_blocks;
 };
 
@@ -108,65 +108,120 @@ __device__ __forceinline__ void rotate_queries(const AppendArgs &a, int64_t wave
     }
 }
 
-// The tokens of one page and head, keys or values: up to kChunks groups of eight a thread.
+// The tokens of one page and head, keys or values: up to kChunks groups of eight a thread stay in registers; of more, which a team
+// of one wave meets where a sequence brings many tokens among many that bring one, all are read a second time.
 constexpr int kChunks = 8;
 
 template <int D, int THREADS, typename T>
-__global__ __launch_bounds__(THREADS) void cache_append_kernel(const AppendArgs a)
+struct PageTokens {
+    const T *in;
+    const float *rotation;  // row of the first token's position; nullptr: not rotated
+    int64_t ld;
+    int groups, rotary;
+    bool interleaved;
+    __device__ __forceinline__ void load(Eight<T> &raw, int i) const
+    {
+        const int g = min(i, groups - 1);
+        raw.load(in + (int64_t)(g / (D / 8)) * ld + 8 * (g % (D / 8)), 8);
+    }
+    __device__ __forceinline__ void get(const Eight<T> &raw, int i, float (&x)[8]) const
+    {
+        // (groups past the end repeat the last one; their partners then are not what they should be: not counted, not stored)
+        raw.get(x);
+        if (rotation) rotate<T>(x, rotation + (int64_t)(min(i, groups - 1) / (D / 8)) * rotary, 8 * (i % (D / 8)), rotary, interleaved);
+    }
+};
+
+__device__ __forceinline__ uint32_t largest(const float (&x)[8])
 {
+    uint32_t v = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v = max(v, magnitude(x[e]));
+    return v;
+}
+
+template <int D>
+__device__ __forceinline__ void store_group(uint8_t *to, int g, const float (&x)[8], float up)
+{
+    uint32_t w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) w[h] = Fp8<false>::pack(x[4 * h] * up, x[4 * h + 1] * up, x[4 * h + 2] * up, x[4 * h + 3] * up);
+    *reinterpret_cast<uint2_t *>(to + 8 * g) = uint2_t{w[0], w[1]};
+}
+
+// THREADS to a team: 64 (four teams to a workgroup), or the workgroup's 256 or 1024
+template <int D, int THREADS, typename T>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void cache_append_kernel(const AppendArgs a)
+{
+    constexpr int kBlock = THREADS < 256 ? 256 : THREADS, kTeams = kBlock / THREADS;
     if (blockIdx.x >= a.append_blocks) {
-        rotate_queries<D, T>(a, (int64_t)(blockIdx.x - a.append_blocks) * (THREADS / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+        rotate_queries<D, T>(a, (int64_t)(blockIdx.x - a.append_blocks) * (kBlock / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
         return;
     }
-    const int tid = threadIdx.x, page_shift = a.t.page_shift, page_size = 1 << page_shift;
-    const bool values = blockIdx.x & 1;
-    const int head = (blockIdx.x >> 1) % a.kv_heads, u = (blockIdx.x >> 1) / a.kv_heads;
-    // Sequence s has the units from cu[s] / page_size + 2 s on: a run of n tokens reaches at most n / page_size + 2 pages.
-    const auto start = [&](int s) { return (first_token(a.t, s) >> page_shift) + 2 * s; };
+    const int tid = kTeams == 1 ? threadIdx.x : threadIdx.x & (THREADS - 1), page_shift = a.t.page_shift, page_size = 1 << page_shift;
+    const int index = kTeams == 1 ? blockIdx.x : blockIdx.x * kTeams + __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
+    const bool values = index & 1;
+    const int u = __builtin_amdgcn_readfirstlane((index >> 1) / a.kv_heads), head = (index >> 1) - u * a.kv_heads;
+    if (kTeams > 1 && a.by_token && u >= a.t.tokens) return;
+    const T *const rows = reinterpret_cast<const T *>(values ? a.v : a.k) + (int64_t)head * D;
+    const int64_t ld = values ? a.ldv : a.ldk;
+    // A unit is a page that new tokens reach.  By token: where `u` is the first new one of its page; its first elements are on
+    // their way before anything else is known.  Else sequence s has the units from cu[s] / page_size + 2 s on: a run of n tokens
+    // reaches at most n / page_size + 2 pages.
+    Eight<T> early;
+    if (a.by_token) early.load(rows + (int64_t)min(u + tid / (D / 8), a.t.tokens - 1) * ld + 8 * (tid % (D / 8)), 8);
+    const auto start = [&](int s) { return a.by_token ? first_token(a.t, s) : (first_token(a.t, s) >> page_shift) + 2 * s; };
     const int s = find_sequence(a.t.sequences, u, start);
     const Sequence q = sequence(a.t, s);
-    const int column = (q.held >> page_shift) + u - start(s);
+    const int column = a.by_token ? (q.held + u - q.first) >> page_shift : (q.held >> page_shift) + u - start(s);
     const int at = column << page_shift;  // position of the page's first slot
     const int last = a.rotary ? min(q.held + q.count, a.positions) : q.held + q.count;
     const int slot0 = max(q.held - at, 0), slot1 = min(last - at, page_size);  // new tokens
-    if (q.count == 0 || slot0 >= slot1) return;
-    const int page = page_at(a.t, s, column);
-    if (page < 0) return;
-    const int first = q.first + at + slot0 - q.held, groups = (slot1 - slot0) * (D / 8);
-    const T *in = reinterpret_cast<const T *>(values ? a.v : a.k) + (int64_t)head * D;
-    const int64_t ld = values ? a.ldv : a.ldk, block = (int64_t)page * a.kv_heads + head;
-    uint8_t *const to = (values ? a.v_pages : a.k_pages) + (block << page_shift) * D;
-    uint8_t *const scale = (values ? a.v_scales : a.k_scales) + block;
+    if (q.count == 0 || slot0 >= slot1 || (a.by_token && u != q.first + at + slot0 - q.held)) return;
     const bool turn = a.rotary && !values;
-
-    Eight<T> raw[kChunks];
+    const PageTokens<D, THREADS, T> tokens{rows + (int64_t)(q.first + at + slot0 - q.held) * ld, turn ? a.rotation + (int64_t)(at + slot0) * a.rotary : nullptr, ld,
+                                           (slot1 - slot0) * (D / 8), a.rotary, a.interleaved};
+    const int groups = tokens.groups;
+    Eight<T> raw[kChunks];  // (on their way before the page is known)
 #pragma unroll
     for (int i = 0; i < kChunks; ++i)
         if (i * THREADS < groups) {
-            const int g = min(tid + i * THREADS, groups - 1);
-            raw[i].load(in + (first + g / (D / 8)) * ld + 8 * (g % (D / 8)), 8);
+            if (i == 0 && a.by_token)
+                raw[0] = early;
+            else
+                tokens.load(raw[i], tid + i * THREADS);
         }
+    const int page = page_at(a.t, s, column);
+    if (page < 0) return;
+    const int64_t block = (int64_t)page * a.kv_heads + head;
+    uint8_t *const to = (values ? a.v_pages : a.k_pages) + (block << page_shift) * D;
+    uint8_t *const scale = (values ? a.v_scales : a.k_scales) + block;
     const int before = slot0 ? *scale : 0;
     float x[kChunks][8];
     uint32_t amax = 0;
 #pragma unroll
     for (int i = 0; i < kChunks; ++i)
         if (i * THREADS < groups) {
-            // (groups past the end repeat the last one; their partners then are not what they should be: not counted)
-            const int g = min(tid + i * THREADS, groups - 1);
-            raw[i].get(x[i]);
-            if (turn) rotate<T>(x[i], a.rotation + (int64_t)(at + slot0 + g / (D / 8)) * a.rotary, 8 * (tid % (D / 8)), a.rotary, a.interleaved);
-            if (tid + i * THREADS < groups)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) amax = max(amax, magnitude(x[i][e]));
+            tokens.get(raw[i], tid + i * THREADS, x[i]);
+            amax = max(amax, tid + i * THREADS < groups ? largest(x[i]) : 0);
         }
+#pragma unroll 1
+    for (int i = kChunks * THREADS; i < groups; i += THREADS) {
+        Eight<T> more;
+        float y[8];
+        tokens.load(more, tid + i);
+        tokens.get(more, tid + i, y);
+        amax = max(amax, tid + i < groups ? largest(y) : 0);
+    }
     amax = group_max_u32<32>(amax);
     amax = max(amax, (uint32_t)__shfl_xor((int)amax, 32));
-    __shared__ uint32_t of_wave[THREADS / kWave];
-    if ((tid & 63) == 0) of_wave[tid >> 6] = amax;
-    __syncthreads();
+    if constexpr (kTeams == 1) {
+        __shared__ uint32_t of_wave[THREADS / kWave];
+        if ((tid & 63) == 0) of_wave[tid >> 6] = amax;
+        __syncthreads();
 #pragma unroll
-    for (int w = 0; w < THREADS / kWave; ++w) amax = max(amax, of_wave[w]);
+        for (int w = 0; w < THREADS / kWave; ++w) amax = max(amax, of_wave[w]);
+    }
 
     // 448 is 1.75 * 2^8
     const int need = amax >= 0x7f800000u ? kNoNumber : max((int)(amax >> 23) - 8 + ((amax & 0x7fffffu) > 0x600000u), 1);
@@ -174,6 +229,7 @@ __global__ __launch_bounds__(THREADS) void cache_append_kernel(const AppendArgs 
     if (tid == 0 && b != before) *scale = (uint8_t)b;
     if (b > before && slot0 && b != kNoNumber) {  // what the page holds goes over to the larger scale
         const float shrink = b - before > 126 ? 0.f : __builtin_bit_cast(float, (uint32_t)(127 - (b - before)) << 23);
+#pragma unroll 1
         for (int i = tid; i < slot0 * (D / 16); i += THREADS) {
             uint4_t w = *reinterpret_cast<const uint4_t *>(to + 16 * i);
 #pragma unroll
@@ -186,35 +242,43 @@ __global__ __launch_bounds__(THREADS) void cache_append_kernel(const AppendArgs 
         }
     }
     const float up = __builtin_bit_cast(float, (uint32_t)max(254 - b, 1) << 23);
+    uint8_t *const new_rows = to + (int64_t)slot0 * D;
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i) {
-        const int g = tid + i * THREADS;
-        if (g < groups) {
-            uint32_t w[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) w[h] = Fp8<false>::pack(x[i][4 * h] * up, x[i][4 * h + 1] * up, x[i][4 * h + 2] * up, x[i][4 * h + 3] * up);
-            *reinterpret_cast<uint2_t *>(to + (int64_t)slot0 * D + 8 * g) = uint2_t{w[0], w[1]};
-        }
+    for (int i = 0; i < kChunks; ++i)
+        if (tid + i * THREADS < groups) store_group<D>(new_rows, tid + i * THREADS, x[i], up);
+#pragma unroll 1
+    for (int i = kChunks * THREADS; i < groups; i += THREADS) {
+        Eight<T> more;
+        float y[8];
+        tokens.load(more, tid + i);
+        tokens.get(more, tid + i, y);
+        if (tid + i < groups) store_group<D>(new_rows, tid + i, y, up);
     }
 }
 
+template <int D, int THREADS, typename T>
+static perf_status launch_append(AppendArgs &a, int64_t units, hipStream_t st)
+{
+    constexpr int kBlock = THREADS < 256 ? 256 : THREADS, kTeams = kBlock / THREADS;
+    const int64_t blocks = (units * a.kv_heads * 2 + kTeams - 1) / kTeams;
+    const int64_t query_blocks = ((int64_t)a.t.tokens * a.q_waves * kWave + kBlock - 1) / kBlock;
+    if (blocks + query_blocks > max_blocks(kBlock)) return PERF_ERR_UNSUPPORTED;
+    a.append_blocks = (uint32_t)blocks;
+    cache_append_kernel<D, THREADS, T><<<(uint32_t)(blocks + query_blocks), kBlock, 0, st>>>(a);
+    return launch_status();
+}
+
+// A wave to a page where a sequence brings about one token (192 sequences, 8 heads of 128: 19.4 us with a workgroup each and two
+// units to a sequence); else as many threads as hold a page's tokens in registers.
 template <int D, typename T>
 static perf_status append(AppendArgs &a, hipStream_t st)
 {
-    const int64_t units = (a.t.tokens >> a.t.page_shift) + 2 * (int64_t)a.t.sequences;
-    const int64_t blocks = units * a.kv_heads * 2;
-    const bool wide = (D << a.t.page_shift) > kChunks * 8 * 256;
-    const int threads = wide ? 1024 : 256;
+    const int64_t by_page = (a.t.tokens >> a.t.page_shift) + 2 * (int64_t)a.t.sequences;
     a.q_waves = a.q ? (int)((a.q_heads * (D / 8) + kWave * kQueryChunks - 1) / (kWave * kQueryChunks)) : 0;
-    const int64_t query_blocks = ((int64_t)a.t.tokens * a.q_waves * kWave + threads - 1) / threads;
-    if (blocks + query_blocks > max_blocks(threads)) return PERF_ERR_UNSUPPORTED;
-    a.append_blocks = (uint32_t)blocks;
-    const dim3 grid((uint32_t)(blocks + query_blocks));
-    if (wide)
-        cache_append_kernel<D, 1024, T><<<grid, 1024, 0, st>>>(a);
-    else
-        cache_append_kernel<D, 256, T><<<grid, 256, 0, st>>>(a);
-    return launch_status();
+    a.by_token = a.t.tokens <= by_page;
+    if (a.by_token) return launch_append<D, 64, T>(a, a.t.tokens, st);
+    if ((D << a.t.page_shift) > kChunks * 8 * 256) return launch_append<D, 1024, T>(a, by_page, st);
+    return launch_append<D, 256, T>(a, by_page, st);
 }
 
 }  // namespace perf

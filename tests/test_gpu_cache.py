@@ -85,6 +85,12 @@ def test_append_many_sequences():
     _check_append([4] * 65, [3] + [0] * 64, 16, 1, 1, 64, BF16, 0)
 
 
+def test_append_a_run_among_single_tokens():
+    """One sequence brings more tokens of a page than a wave holds in registers."""
+    for dt in (BF16, F32):
+        _check_append([5] * 40 + [3] + [9] * 30, [1] * 40 + [60] + [1] * 30, 256, 2, 1, 256, dt, 256)
+
+
 def test_append_positions_and_pages_that_are_not_there():
     """Positions behind the rotation's end, columns behind the table's, entries that are no page."""
     _check_append([0, 30, 70, 100], [90, 60, 1, 2], 16, 2, 1, 64, BF16, 64, positions=75)
