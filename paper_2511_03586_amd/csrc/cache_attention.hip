@@ -204,16 +204,45 @@ __device__ __forceinline__ Place find_place(PlaceScratch &at, int items, int cop
     return p;
 }
 
-// What has to be joined where the run of `worker` begins, in a tile of rows whose `tiles` begin with `start`
+// A tile of rows takes kSetup places of the list before those of its tiles of keys: what a workgroup spends on its beginning and
+// end, about as long as on that many tiles of 128 keys.  (With none, 64 sequences of 64 to 32768 tokens took 165 us where 64 of
+// 5242 took 125: workgroups that met short sequences met many.)
+constexpr int kSetup = 3;
+
+// What has to be joined where the run of `worker` begins, in a tile of rows whose places, kSetup and `tiles`, begin with `start`
 __device__ __forceinline__ Join join_at(const Place &p, int worker, int workers, int64_t start, int tiles, Join j)
 {
     j.count = 0, j.from = worker - 1, j.odd = 0, j.unused = 0;
-    if (start < p.start && start >= run_start(p.total, worker - 1, workers)) {
-        j.count = worker_of(p.total, start + tiles - 1, workers) - j.from + 1;
-        j.odd = run_start(p.total, worker - 1, workers) < start;
+    const int64_t before = worker ? run_start(p.total, worker - 1, workers) : 0, first = start + kSetup;
+    if (worker && first < p.start && first >= before) {
+        j.count = worker_of(p.total, first + tiles - 1, workers) - j.from + 1;
+        j.odd = before < start;
     }
     return j;
 }
+
+// The sequences' first tokens and lengths in LDS, where they fit
+constexpr int kSequencesInLds = 1024;
+constexpr int kSequencesBytes = (2 * kSequencesInLds + 1) * 4;
+struct Sequences {
+    const AttentionArgs &a;
+    int *firsts, *lengths;
+    bool in_lds;
+    __device__ __forceinline__ Sequences(const AttentionArgs &args, char *lds) : a(args), firsts(reinterpret_cast<int *>(lds)), lengths(firsts + kSequencesInLds + 1)
+    {
+        in_lds = a.t.sequences <= kSequencesInLds;
+        if (in_lds) {
+            for (int i = threadIdx.x; i <= a.t.sequences; i += 256) firsts[i] = first_token(a.t, i);
+            for (int i = threadIdx.x; i < a.t.sequences; i += 256) lengths[i] = a.t.lengths[i];
+            __syncthreads();
+        }
+    }
+    __device__ __forceinline__ int first(int s) const { return in_lds ? firsts[s] : first_token(a.t, s); }
+    __device__ __forceinline__ Span span(int s) const
+    {
+        return in_lds ? perf::span(a, sequence(firsts[s], firsts[s + 1], lengths[s])) : perf::span(a, s);
+    }
+};
 
 // ---- few rows: up to 16 of (token, head of a group) ---------------------------------------------------------------------
 // Decoding: bound by the bytes of the cache.  The keys of all sequences and heads, in tiles of 128, are one list that is cut into
@@ -227,7 +256,8 @@ __device__ __forceinline__ Join join_at(const Place &p, int worker, int workers,
 constexpr int kFewRows = 16, kFewWaves = 4, kFewKeys = 32 * kFewWaves;
 
 template <int D> constexpr int few_stages() { return D == 64 ? 4 : 2; }
-template <int D> constexpr int few_lds() { return kFewWaves * few_stages<D>() * 64 * D; }
+template <int D> constexpr int few_ring() { return kFewWaves * few_stages<D>() * 64 * D; }
+template <int D> constexpr int few_lds() { return few_ring<D>() + kSequencesBytes; }
 template <int D> constexpr int few_workers() { return D == 256 ? 256 : 512; }  // as many as are on the chip at a time
 constexpr int partial_floats(int rows, int D) { return rows * (D + 2); }  // sums of a tile of rows, maxima, sums of weights
 
@@ -248,12 +278,15 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, col = lane & 15;
     const int worker = blockIdx.x, group = uniform(a.q_heads / a.kv_heads), shift = a.t.page_shift, in_page = (1 << shift) - 1;
+    const Sequences sequences(a, smem + few_ring<D>());
     const Place place = find_place(*reinterpret_cast<PlaceScratch *>(smem), a.t.sequences, 1, worker, gridDim.x, [&](int i, int to, auto &&take) {
-                                       for (; i < to; ++i) take(i, few_tiles(a, span(a, i)) * a.kv_heads);
-                                   });
-    int64_t x = place.start;
+        for (; i < to; ++i) {
+            const int tiles = few_tiles(a, sequences.span(i));
+            take(i, tiles ? (kSetup + tiles) * a.kv_heads : 0);
+        }
+    });
     const int64_t stop = place.stop;
-    if (x >= stop) {
+    if (place.start >= stop) {
         if (tid == 0) a.few_join[worker].count = 0;
         return;
     }
@@ -279,18 +312,66 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
     const float sign = a.scale > 0.f ? 1.f : a.scale < 0.f ? -1.f : 0.f, c = log2_scale(a);
 
     int s = place.item;
-    Span r = uniform(span(a, s));
+    Span r = uniform(sequences.span(s));
     int tiles = few_tiles(a, r);
-    int head = uniform((int)((x - place.before) / tiles)), t0 = uniform((int)((x - place.before) - (int64_t)head * tiles));
+    int head = uniform((int)((place.start - place.before) / (kSetup + tiles)));
+    int64_t start = place.before + (int64_t)head * (kSetup + tiles);  // of the head's places
+    int t0 = uniform((int)max(place.start - start - kSetup, (int64_t)0));
     if (tid == 0)
-        a.few_join[worker] = join_at(place, worker, workers_of(place.total, gridDim.x), x - t0, tiles, Join{0, 0, 0, r.q.first, 0, r.q.count * group, head, 0});
+        a.few_join[worker] = join_at(place, worker, workers_of(place.total, gridDim.x), start, tiles, Join{0, 0, 0, r.q.first, 0, r.q.count * group, head, 0});
     bool first = true;
-    while (x < stop) {
-        const int n = uniform((int)min((int64_t)(tiles - t0), stop - x)), rows = r.q.count * group;
-        const int held = r.q.held, end = r.end, from = r.begin + t0 * kFewKeys + 32 * wave;  // this wave's first key
+
+    // Pages and scales of 64 blocks, one a lane: those of block i are in lane i % 64
+    int page0, page1, n, from;
+    uint32_t scales;  // bytes: K and V of the first half, K and V of the second
+    const auto look_up_pages = [&](int base) {
+        const int i = base + lane, k = from + i * kFewKeys;
+        page0 = i < n && k < r.end ? page_at(a.t, s, k >> shift) : -1;
+        page1 = i < n && k + 16 < r.end ? page_at(a.t, s, (k + 16) >> shift) : -1;
+    };
+    const auto look_up_scales = [&] {
+        uint32_t b[4] = {0, 0, 0, 0};
+        if (page0 >= 0) b[0] = a.k_scales[(int64_t)page0 * a.kv_heads + head], b[1] = a.v_scales[(int64_t)page0 * a.kv_heads + head];
+        if (page1 >= 0) b[2] = a.k_scales[(int64_t)page1 * a.kv_heads + head], b[3] = a.v_scales[(int64_t)page1 * a.kv_heads + head];
+        scales = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
+    };
+    // the run's tiles of this head, and the pages that this wave meets first
+    const auto begin = [&] {
+        n = uniform((int)min((int64_t)(tiles - t0), stop - (start + kSetup + t0)));
+        from = r.begin + t0 * kFewKeys + 32 * wave;
+        if (n > 0) look_up_pages(0);
+    };
+    begin();
+    while (n > 0) {
+        const int rows = r.q.count * group, held = r.q.held, end = r.end;
+        const int token = col / group, position = held + token, last = held + r.q.count - 1;
+        asm volatile("" : "+v"(page0), "+v"(page1));
+
+        struct Block { uint32_t scales; int pages; };  // pages: bit h: half h is there
+        const auto block_of = [&](int i) {
+            return Block{(uint32_t)__builtin_amdgcn_readlane((int)scales, i & 63),
+                         (__builtin_amdgcn_readlane(page0, i & 63) >= 0 ? 1 : 0) | (__builtin_amdgcn_readlane(page1, i & 63) >= 0 ? 2 : 0)};
+        };
+        auto issue = [&](int i) {  // (blocks past the end move nothing: the number in flight stays the same)
+            const int p0 = __builtin_amdgcn_readlane(page0, i & 63), p1 = __builtin_amdgcn_readlane(page1, i & 63);
+            const int k = from + i * kFewKeys;
+            char *const to = ring + (i % kStages) * kStage;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int p = h ? p1 : p0;
+                const rsrc_t in_k = block_rsrc(a.k_pages, a, p, head, D), in_v = block_rsrc(a.v_pages, a, p, head, D);
+                const uint32_t at = (uint32_t)((k + 16 * h) & in_page) * D;
+#pragma unroll
+                for (int j = h * kLoads / 4; j < (h + 1) * kLoads / 4; ++j) issue_load_to(in_k, off_k[j], at, to + j * 1024);
+#pragma unroll
+                for (int j = h * kLoads / 4; j < (h + 1) * kLoads / 4; ++j) issue_load_to(in_v, off_v[j], at, to + (kLoads / 2 + j) * 1024);
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < kStages; ++i) issue(i);
+        look_up_scales();
 
         // this lane's query (columns without one repeat another)
-        const int token = col / group, position = held + token, last = held + r.q.count - 1;
         bf16x8_t q[D / 32][kQ];
         {
             const T *row = reinterpret_cast<const T *>(a.q) + (int64_t)(r.q.first + min(token, r.q.count - 1)) * a.ldq + (int64_t)(head * group + col % group) * D;
@@ -306,39 +387,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
                 split_eight(v, q[i]);
             }
         }
-
-        // Pages and scales of 64 blocks, one a lane: those of block i are in lane i % 64
-        int page0 = -1, page1 = -1;
-        uint32_t scales = 0;  // bytes: K and V of the first half, K and V of the second
-        auto look_up = [&](int base) {
-            const int i = base + lane, k = from + i * kFewKeys;
-            page0 = i < n && k < end ? page_at(a.t, s, k >> shift) : -1;
-            page1 = i < n && k + 16 < end ? page_at(a.t, s, (k + 16) >> shift) : -1;
-            uint32_t b[4] = {0, 0, 0, 0};
-            if (page0 >= 0) b[0] = a.k_scales[(int64_t)page0 * a.kv_heads + head], b[1] = a.v_scales[(int64_t)page0 * a.kv_heads + head];
-            if (page1 >= 0) b[2] = a.k_scales[(int64_t)page1 * a.kv_heads + head], b[3] = a.v_scales[(int64_t)page1 * a.kv_heads + head];
-            scales = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
-            wait_vmem<0>();
-            asm volatile("" : "+v"(page0), "+v"(page1), "+v"(scales));
-        };
-        struct Block { uint32_t scales; int pages; };  // pages: bit h: half h is there
-        auto issue = [&](int i) {  // (blocks past the end move nothing: the number in flight stays the same)
-            if ((i & 63) == 0) look_up(i);
-            const int p0 = __builtin_amdgcn_readlane(page0, i & 63), p1 = __builtin_amdgcn_readlane(page1, i & 63);
-            const int k = from + i * kFewKeys;
-            char *const to = ring + (i % kStages) * kStage;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int p = h ? p1 : p0;
-                const rsrc_t in_k = block_rsrc(a.k_pages, a, p, head, D), in_v = block_rsrc(a.v_pages, a, p, head, D);
-                const uint32_t at = (uint32_t)((k + 16 * h) & in_page) * D;
-#pragma unroll
-                for (int j = h * kLoads / 4; j < (h + 1) * kLoads / 4; ++j) issue_load_to(in_k, off_k[j], at, to + j * 1024);
-#pragma unroll
-                for (int j = h * kLoads / 4; j < (h + 1) * kLoads / 4; ++j) issue_load_to(in_v, off_v[j], at, to + (kLoads / 2 + j) * 1024);
-            }
-            return Block{(uint32_t)__builtin_amdgcn_readlane((int)scales, i & 63), (p0 >= 0 ? 1 : 0) | (p1 >= 0 ? 2 : 0)};
-        };
+        wait_vmem<0>();
+        asm volatile("" : "+v"(scales));
 
         float4_t o[D / 16];
 #pragma unroll
@@ -346,7 +396,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
         float m = -INFINITY, l = 0.f;
         Block ahead[kStages];
 #pragma unroll
-        for (int i = 0; i < kStages; ++i) ahead[i] = issue(i);
+        for (int i = 0; i < kStages; ++i) ahead[i] = block_of(i);
         int stage = 0;
         for (int i = 0; i < n; ++i) {
             wait_vmem<(kStages - 1) * kLoads>();
@@ -366,7 +416,14 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
             const Block now = ahead[0];
 #pragma unroll
             for (int j = 0; j + 1 < kStages; ++j) ahead[j] = ahead[j + 1];
-            ahead[kStages - 1] = issue(i + kStages);
+            if (((i + kStages) & 63) == 0) {
+                look_up_pages(i + kStages);
+                look_up_scales();
+                wait_vmem<0>();
+                asm volatile("" : "+v"(page0), "+v"(page1), "+v"(scales));
+            }
+            issue(i + kStages);
+            ahead[kStages - 1] = block_of(i + kStages);
             stage = stage + kStage == kStages * kStage ? 0 : stage + kStage;
             const int k = from + i * kFewKeys;
             if (k >= end) continue;
@@ -436,9 +493,21 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) *reinterpret_cast<float4_t *>(mine + col * kRow + 16 * d + 4 * g) = o[d];
         if (lane < kFewRows) mine[kFewRows * kRow + lane] = m, mine[kFewRows * kRow + kFewRows + lane] = l;
-        __syncthreads();
         const bool whole = n == tiles;
         float *const out = whole ? nullptr : a.few_partial + (int64_t)(2 * worker + !first) * partial_floats(kFewRows, D);
+        const int of_token = r.q.first, of_head = head * group;
+        first = false;
+        // the next head's first pages are on their way while this one's sums are joined
+        start += kSetup + tiles, t0 = 0;
+        if (start < stop) {
+            if (++head == a.kv_heads) {
+                head = 0;
+                do r = uniform(sequences.span(++s)), tiles = few_tiles(a, r);
+                while (tiles == 0);
+            }
+        }
+        begin();
+        __syncthreads();
         for (int i = tid; i < rows * (D / 4); i += 256) {
             const int row = i / (D / 4), d = 4 * (i % (D / 4));
             float mw[kFewWaves], top = -INFINITY, sum = 0.f;
@@ -457,20 +526,13 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
                 sum += f * of[kFewRows * kRow + kFewRows + row];
             }
             if (whole) {
-                finish<T>(a, r.q.first + row / group, head * group + row % group, d, D, v, top, sum);
+                finish<T>(a, of_token + row / group, of_head + row % group, d, D, v, top, sum);
             } else {
                 *reinterpret_cast<float4_t *>(out + row * D + d) = v;
                 if (d == 0) out[kFewRows * D + row] = top, out[kFewRows * (D + 1) + row] = sum;
             }
         }
         __syncthreads();
-        first = false;
-        x += n, t0 = 0;
-        if (x < stop && ++head == a.kv_heads) {
-            head = 0;
-            do r = uniform(span(a, ++s)), tiles = few_tiles(a, r);
-            while (tiles == 0);
-        }
     }
 }
 
@@ -490,8 +552,7 @@ template <int D> constexpr int many_rows() { return 128 * many_tiles<D>(); }
 // workgroups to a CU: one where a wave needs more than 256 registers (its queries and sums)
 template <int D, typename T> constexpr int many_per_cu() { return D == 256 || (D == 128 && sizeof(T) == 4) ? 1 : 2; }
 template <int D, typename T> constexpr int many_workers() { return 256 * many_per_cu<D, T>(); }
-constexpr int kSequencesInLds = 1024;
-template <int D> constexpr int many_lds() { return kManyStages * 2 * kManyKeys * D + (2 * kSequencesInLds + 1) * 4; }
+template <int D> constexpr int many_lds() { return kManyStages * 2 * kManyKeys * D + kSequencesBytes; }
 
 template <int D> __device__ __forceinline__ constexpr int turn_many_v(int r)
 {
@@ -530,35 +591,23 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
     const int group = uniform(a.q_heads / a.kv_heads), shift = a.t.page_shift, in_page = (1 << shift) - 1, sequences = a.t.sequences;
     const int worker = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);  // (a multiple of 8 workgroups)
 
-    // the sequences' first tokens and lengths, where they fit
-    int *const firsts = reinterpret_cast<int *>(smem + kManyStages * kStage), *const lengths = firsts + kSequencesInLds + 1;
-    const bool in_lds = sequences <= kSequencesInLds;
-    if (in_lds) {
-        for (int i = tid; i <= sequences; i += 256) firsts[i] = first_token(a.t, i);
-        for (int i = tid; i < sequences; i += 256) lengths[i] = a.t.lengths[i];
-        __syncthreads();
-    }
-    const auto first_of = [&](int s) { return in_lds ? firsts[s] : first_token(a.t, s); };
-    const auto start_of = [&](int s) { return many_start(first_of(s), group, kRows, s); };
-    const auto span_of = [&](int s) {
-        return in_lds ? span(a, sequence(firsts[s], firsts[s + 1], lengths[s])) : span(a, s);
-    };
-    const Place place = find_place(*reinterpret_cast<PlaceScratch *>(smem), units, a.kv_heads, worker, gridDim.x,
-                                   [&](int u, int to, auto &&take) {
-                                       if (u >= to) return;
-                                       int s = 0;  // the last sequence that begins at u or before
-                                       for (int n = sequences; n > 1;) {
-                                           const int half = n >> 1;
-                                           if (start_of(s + half) <= u) s += half, n -= half; else n = half;
-                                       }
-                                       for (; u < to; ++u) {
-                                           while (s + 1 < sequences && start_of(s + 1) <= u) ++s;
-                                           take(u, many_keys(a, span_of(s), group, u - start_of(s), kRows).tiles);
-                                       }
-                                   });
-    int64_t x = place.start;
+    const Sequences all(a, smem + kManyStages * kStage);
+    const auto start_of = [&](int s) { return many_start(all.first(s), group, kRows, s); };
+    const Place place = find_place(*reinterpret_cast<PlaceScratch *>(smem), units, a.kv_heads, worker, gridDim.x, [&](int u, int to, auto &&take) {
+        if (u >= to) return;
+        int s = 0;  // the last sequence that begins at u or before
+        for (int n = sequences; n > 1;) {
+            const int half = n >> 1;
+            if (start_of(s + half) <= u) s += half, n -= half; else n = half;
+        }
+        for (; u < to; ++u) {
+            while (s + 1 < sequences && start_of(s + 1) <= u) ++s;
+            const int tiles = many_keys(a, all.span(s), group, u - start_of(s), kRows).tiles;
+            take(u, tiles ? kSetup + tiles : 0);
+        }
+    });
     const int64_t stop = place.stop;
-    if (x >= stop) {
+    if (place.start >= stop) {
         if (tid == 0) a.many_join[worker].count = 0;
         return;
     }
@@ -583,17 +632,18 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
 
     int head = place.copy, u = place.item;
     int s = find_sequence(sequences, u, start_of);
-    Span r = uniform(span_of(s));
+    Span r = uniform(all.span(s));
     int tile = u - uniform(start_of(s));
-    int t0 = uniform((int)(x - head * (place.total / a.kv_heads) - place.before));
+    int64_t start = head * (place.total / a.kv_heads) + place.before;  // of the row tile's places
+    int t0 = uniform((int)max(place.start - start - kSetup, (int64_t)0));
     if (tid == 0)
-        a.many_join[worker] = join_at(place, worker, workers_of(place.total, gridDim.x), x - t0, many_keys(a, r, group, tile, kRows).tiles,
+        a.many_join[worker] = join_at(place, worker, workers_of(place.total, gridDim.x), start, many_keys(a, r, group, tile, kRows).tiles,
                                       Join{0, 0, 0, r.q.first, tile * kRows, min(r.q.count * group - tile * kRows, kRows), head, 0});
     bool first = true;
     while (true) {
         const Keys keys = uniform(many_keys(a, r, group, tile, kRows));
-        const int n = uniform((int)min((int64_t)(keys.tiles - t0), stop - x)), rows = r.q.count * group;
-        if (n < 1) return;  // (only where cu does not ascend)
+        const int n = uniform((int)min((int64_t)(keys.tiles - t0), stop - (start + kSetup + t0))), rows = r.q.count * group;
+        if (n < 1) return;
         const int held = r.q.held, end = keys.end, from = keys.begin + t0 * kManyKeys;
         const int row0 = tile * kRows + 32 * kTiles * wave;  // this wave's first row
         const bool active = row0 < rows;
@@ -822,16 +872,16 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
             }
         }
         first = false;
-        x += n, t0 = 0;
-        if (x >= stop) break;
+        start += kSetup + keys.tiles, t0 = 0;
+        if (start >= stop) break;
         // the next row tile that has keys
         do {
             if (++u == units) {
                 u = 0, s = 0;
                 if (++head == a.kv_heads) return;  // (only where cu does not ascend)
-                r = uniform(span_of(s));
+                r = uniform(all.span(s));
             }
-            while (s + 1 < sequences && uniform(start_of(s + 1)) <= u) r = uniform(span_of(++s));
+            while (s + 1 < sequences && uniform(start_of(s + 1)) <= u) r = uniform(all.span(++s));
             tile = u - uniform(start_of(s));
         } while (uniform(many_keys(a, r, group, tile, kRows)).tiles == 0);
     }
