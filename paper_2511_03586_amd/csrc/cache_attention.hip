@@ -16,6 +16,7 @@ struct AttentionArgs {
     float *lse;
     int64_t ldq, ldo;
     int q_heads, kv_heads, max_tokens, window;
+    uint32_t group_magic;  // of div_by: rows of a sequence are (token, head of its group)
     float scale;
     // scratch of the kernels for few and for many rows: what is to be joined, and the sums that workgroups leave
     struct Join *few_join, *many_join;
@@ -40,6 +41,17 @@ __device__ __forceinline__ void finish(const AttentionArgs &a, int token, int he
     store_row_chunk<true, T, 4>(o, w);
     if (a.lse && d == 0) a.lse[(int64_t)token * a.q_heads + head] = __builtin_fmaf(top, fabsf(a.scale), logf(sum));
 }
+
+template <typename T>
+__device__ __forceinline__ void finish_eight(const AttentionArgs &a, int token, int head, int d, int D, float4_t lo, float4_t hi, float top, float sum)
+{
+    const float r = sum == 0.f ? 0.f : 1.0f / sum;
+    const float w[8] = {lo[0] * r, lo[1] * r, lo[2] * r, lo[3] * r, hi[0] * r, hi[1] * r, hi[2] * r, hi[3] * r};
+    store_row_chunk<true, T, 8>(reinterpret_cast<T *>(a.o) + (int64_t)token * a.ldo + (int64_t)head * D + d, w);
+    if (a.lse && d == 0) a.lse[(int64_t)token * a.q_heads + head] = __builtin_fmaf(top, fabsf(a.scale), logf(sum));
+}
+
+__device__ __forceinline__ int token_of(const AttentionArgs &a, int row, int group) { return div_by(row, group, a.group_magic); }
 
 // ---- what both kernels share ----------------------------------------------------------------------------------------------
 
@@ -73,6 +85,26 @@ __device__ __forceinline__ void split_eight(const float (&x)[8], bf16x8_t (&part
             left -= (float)part[n][e];
         }
     }
+}
+
+// Transposing loads from LDS (ds_read_b64_tr_b8: of 16 lanes, whose addresses are those of eight rows' halves, lane c gets column c),
+// four of them: at four addresses, or at one and kStep, 2 kStep, 3 kStep behind it.  Written out, and waited for at once, because
+// in front of the builtin the compiler waits for every load into LDS that is on its way.
+__device__ __forceinline__ uint32_t lds_address(const char *p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)p; }
+__device__ __forceinline__ void read_transposed(int2v_t *to, uint32_t at0, uint32_t at1, uint32_t at2, uint32_t at3)
+{
+    asm volatile("ds_read_b64_tr_b8 %0, %4\n\tds_read_b64_tr_b8 %1, %5\n\tds_read_b64_tr_b8 %2, %6\n\tds_read_b64_tr_b8 %3, %7\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(to[0]), "=&v"(to[1]), "=&v"(to[2]), "=&v"(to[3])
+                 : "v"(at0), "v"(at1), "v"(at2), "v"(at3)
+                 : "memory");
+}
+template <int kStep>
+__device__ __forceinline__ void read_transposed(int2v_t *to, uint32_t at)
+{
+    asm volatile("ds_read_b64_tr_b8 %0, %4\n\tds_read_b64_tr_b8 %1, %4 offset:%5\n\tds_read_b64_tr_b8 %2, %4 offset:%6\n\tds_read_b64_tr_b8 %3, %4 offset:%7\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(to[0]), "=&v"(to[1]), "=&v"(to[2]), "=&v"(to[3])
+                 : "v"(at), "n"(kStep), "n"(2 * kStep), "n"(3 * kStep)
+                 : "memory");
 }
 
 // Values that are the same in all lanes, in scalar registers
@@ -204,16 +236,16 @@ __device__ __forceinline__ Place find_place(PlaceScratch &at, int items, int cop
     return p;
 }
 
-// A tile of rows takes kSetup places of the list before those of its tiles of keys: what a workgroup spends on its beginning and
-// end, about as long as on that many tiles of 128 keys.  (With none, 64 sequences of 64 to 32768 tokens took 165 us where 64 of
-// 5242 took 125: workgroups that met short sequences met many.)
-constexpr int kSetup = 3;
+// A tile of rows takes some places of the list before those of its tiles of keys: what a workgroup spends on its beginning and
+// end, in tiles of keys.  (With none, 64 sequences of 64 to 32768 tokens took 165 us where 64 of 5242 took 125: workgroups that
+// met short sequences met many.)
+constexpr int kFewSetup = 3, kManySetup = 5;
 
-// What has to be joined where the run of `worker` begins, in a tile of rows whose places, kSetup and `tiles`, begin with `start`
-__device__ __forceinline__ Join join_at(const Place &p, int worker, int workers, int64_t start, int tiles, Join j)
+// What has to be joined where the run of `worker` begins, in a tile of rows whose places, `setup` and `tiles`, begin with `start`
+__device__ __forceinline__ Join join_at(const Place &p, int worker, int workers, int64_t start, int setup, int tiles, Join j)
 {
     j.count = 0, j.from = worker - 1, j.odd = 0, j.unused = 0;
-    const int64_t before = worker ? run_start(p.total, worker - 1, workers) : 0, first = start + kSetup;
+    const int64_t before = worker ? run_start(p.total, worker - 1, workers) : 0, first = start + setup;
     if (worker && first < p.start && first >= before) {
         j.count = worker_of(p.total, first + tiles - 1, workers) - j.from + 1;
         j.odd = before < start;
@@ -222,7 +254,7 @@ __device__ __forceinline__ Join join_at(const Place &p, int worker, int workers,
 }
 
 // The sequences' first tokens and lengths in LDS, where they fit
-constexpr int kSequencesInLds = 1024;
+constexpr int kSequencesInLds = 512;
 constexpr int kSequencesBytes = (2 * kSequencesInLds + 1) * 4;
 struct Sequences {
     const AttentionArgs &a;
@@ -282,7 +314,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
     const Place place = find_place(*reinterpret_cast<PlaceScratch *>(smem), a.t.sequences, 1, worker, gridDim.x, [&](int i, int to, auto &&take) {
         for (; i < to; ++i) {
             const int tiles = few_tiles(a, sequences.span(i));
-            take(i, tiles ? (kSetup + tiles) * a.kv_heads : 0);
+            take(i, tiles ? (kFewSetup + tiles) * a.kv_heads : 0);
         }
     });
     const int64_t stop = place.stop;
@@ -314,11 +346,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
     int s = place.item;
     Span r = uniform(sequences.span(s));
     int tiles = few_tiles(a, r);
-    int head = uniform((int)((place.start - place.before) / (kSetup + tiles)));
-    int64_t start = place.before + (int64_t)head * (kSetup + tiles);  // of the head's places
-    int t0 = uniform((int)max(place.start - start - kSetup, (int64_t)0));
+    int head = uniform((int)((place.start - place.before) / (kFewSetup + tiles)));
+    int64_t start = place.before + (int64_t)head * (kFewSetup + tiles);  // of the head's places
+    int t0 = uniform((int)max(place.start - start - kFewSetup, (int64_t)0));
     if (tid == 0)
-        a.few_join[worker] = join_at(place, worker, workers_of(place.total, gridDim.x), start, tiles, Join{0, 0, 0, r.q.first, 0, r.q.count * group, head, 0});
+        a.few_join[worker] = join_at(place, worker, workers_of(place.total, gridDim.x), start, kFewSetup, tiles, Join{0, 0, 0, r.q.first, 0, r.q.count * group, head, 0});
     bool first = true;
 
     // Pages and scales of 64 blocks, one a lane: those of block i are in lane i % 64
@@ -337,14 +369,14 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
     };
     // the run's tiles of this head, and the pages that this wave meets first
     const auto begin = [&] {
-        n = uniform((int)min((int64_t)(tiles - t0), stop - (start + kSetup + t0)));
+        n = uniform((int)min((int64_t)(tiles - t0), stop - (start + kFewSetup + t0)));
         from = r.begin + t0 * kFewKeys + 32 * wave;
         if (n > 0) look_up_pages(0);
     };
     begin();
     while (n > 0) {
         const int rows = r.q.count * group, held = r.q.held, end = r.end;
-        const int token = col / group, position = held + token, last = held + r.q.count - 1;
+        const int token = token_of(a, col, group), position = held + token, last = held + r.q.count - 1;
         asm volatile("" : "+v"(page0), "+v"(page1));
 
         struct Block { uint32_t scales; int pages; };  // pages: bit h: half h is there
@@ -374,7 +406,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
         // this lane's query (columns without one repeat another)
         bf16x8_t q[D / 32][kQ];
         {
-            const T *row = reinterpret_cast<const T *>(a.q) + (int64_t)(r.q.first + min(token, r.q.count - 1)) * a.ldq + (int64_t)(head * group + col % group) * D;
+            const T *row = reinterpret_cast<const T *>(a.q) + (int64_t)(r.q.first + min(token, r.q.count - 1)) * a.ldq + (int64_t)(head * group + col - token * group) * D;
             Eight<T> raw[D / 32];
 #pragma unroll
             for (int i = 0; i < D / 32; ++i) raw[i].load_cached(row + 64 * (i >> 1) + 16 * g + 8 * (i & 1), 8);
@@ -408,9 +440,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int j = 0; j < D / 64; ++j) raw_k[h][j] = *reinterpret_cast<const int4v_t *>(ring + stage + at_k[h][j]);
+            const uint32_t in_stage = lds_address(ring) + stage;
 #pragma unroll
-            for (int d = 0; d < D / 16; ++d)
-                raw_v[d] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) int2v_t *)(ring + stage + at_v[d]));
+            for (int d = 0; d < D / 16; d += 4)
+                read_transposed(raw_v + d, in_stage + at_v[d], in_stage + at_v[d + 1], in_stage + at_v[d + 2], in_stage + at_v[d + 3]);
             wait_lds();
             fence();
             const Block now = ahead[0];
@@ -498,7 +531,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
         const int of_token = r.q.first, of_head = head * group;
         first = false;
         // the next head's first pages are on their way while this one's sums are joined
-        start += kSetup + tiles, t0 = 0;
+        start += kFewSetup + tiles, t0 = 0;
         if (start < stop) {
             if (++head == a.kv_heads) {
                 head = 0;
@@ -526,7 +559,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
                 sum += f * of[kFewRows * kRow + kFewRows + row];
             }
             if (whole) {
-                finish<T>(a, of_token + row / group, of_head + row % group, d, D, v, top, sum);
+                finish<T>(a, of_token + token_of(a, row, group), of_head + row - token_of(a, row, group) * group, d, D, v, top, sum);
             } else {
                 *reinterpret_cast<float4_t *>(out + row * D + d) = v;
                 if (d == 0) out[kFewRows * D + row] = top, out[kFewRows * (D + 1) + row] = sum;
@@ -547,12 +580,13 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
 // of them): another product with what that leaves would cost half of the time again.  A running maximum is raised only by more
 // than 2^8 in weights, which fp32 sums carry as well: the sums are then seldom scaled.
 constexpr int kManyKeys = 64, kManyStages = 3;
-template <int D> constexpr int many_tiles() { return 1; }
-template <int D> constexpr int many_rows() { return 128 * many_tiles<D>(); }
-// workgroups to a CU: one where a wave needs more than 256 registers (its queries and sums)
-template <int D, typename T> constexpr int many_per_cu() { return D == 256 || (D == 128 && sizeof(T) == 4) ? 1 : 2; }
+constexpr int kManyRows = 128;
+// workgroups to a CU, by the registers that a wave needs for its queries and sums
+template <int D, typename T> constexpr int many_per_cu() { return D == 256 || (D == 128 && sizeof(T) == 4) ? 1 : D == 64 && sizeof(T) == 2 ? 3 : 2; }
 template <int D, typename T> constexpr int many_workers() { return 256 * many_per_cu<D, T>(); }
-template <int D> constexpr int many_lds() { return kManyStages * 2 * kManyKeys * D + kSequencesBytes; }
+// (three stages; for heads of 64 a little more, which the sums need on their way out)
+template <int D> constexpr int many_ring() { return std::max(kManyStages * 2 * kManyKeys * D, 4 * (32 * 68 + 64) * 4); }
+template <int D> constexpr int many_lds() { return many_ring<D>() + kSequencesBytes; }
 
 template <int D> __device__ __forceinline__ constexpr int turn_many_v(int r)
 {
@@ -573,7 +607,7 @@ __device__ __forceinline__ Keys many_keys(const AttentionArgs &a, const Span &r,
     const int rows = r.q.count * group, row = tile * tile_rows;
     Keys k{0, 0, 0};
     if (row >= rows || is_few(a, r.q.count)) return k;
-    const int token0 = row / group, token1 = (min(row + tile_rows, rows) - 1) / group;
+    const int token0 = token_of(a, row, group), token1 = token_of(a, min(row + tile_rows, rows) - 1, group);
     k.end = (int)min((int64_t)r.q.held + token1 + 1, (int64_t)a.t.columns << a.t.page_shift);
     k.begin = a.window ? max(r.q.held + token0 - a.window + 1, 0) & ~(kManyKeys - 1) : 0;
     k.tiles = max((k.end - k.begin + kManyKeys - 1) / kManyKeys, 1);
@@ -585,13 +619,13 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
 {
     constexpr int kStage = 2 * kManyKeys * D, kLoads = D / 32;                  // loads of a wave and block: K, then V
     constexpr int kQ = sizeof(T) == 4 ? 3 : 1, kP = sizeof(T) == 4 ? 3 : 1;     // bf16 parts of a query's element and of a weight
-    constexpr int kTiles = many_tiles<D>(), kRows = many_rows<D>();
+    constexpr int kRows = kManyRows;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, col = lane & 31;
     const int group = uniform(a.q_heads / a.kv_heads), shift = a.t.page_shift, in_page = (1 << shift) - 1, sequences = a.t.sequences;
     const int worker = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);  // (a multiple of 8 workgroups)
 
-    const Sequences all(a, smem + kManyStages * kStage);
+    const Sequences all(a, smem + many_ring<D>());
     const auto start_of = [&](int s) { return many_start(all.first(s), group, kRows, s); };
     const Place place = find_place(*reinterpret_cast<PlaceScratch *>(smem), units, a.kv_heads, worker, gridDim.x, [&](int u, int to, auto &&take) {
         if (u >= to) return;
@@ -603,7 +637,7 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
         for (; u < to; ++u) {
             while (s + 1 < sequences && start_of(s + 1) <= u) ++s;
             const int tiles = many_keys(a, all.span(s), group, u - start_of(s), kRows).tiles;
-            take(u, tiles ? kSetup + tiles : 0);
+            take(u, tiles ? kManySetup + tiles : 0);
         }
     });
     const int64_t stop = place.stop;
@@ -635,41 +669,71 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
     Span r = uniform(all.span(s));
     int tile = u - uniform(start_of(s));
     int64_t start = head * (place.total / a.kv_heads) + place.before;  // of the row tile's places
-    int t0 = uniform((int)max(place.start - start - kSetup, (int64_t)0));
+    int t0 = uniform((int)max(place.start - start - kManySetup, (int64_t)0));
+    Keys keys = uniform(many_keys(a, r, group, tile, kRows));
     if (tid == 0)
-        a.many_join[worker] = join_at(place, worker, workers_of(place.total, gridDim.x), start, many_keys(a, r, group, tile, kRows).tiles,
+        a.many_join[worker] = join_at(place, worker, workers_of(place.total, gridDim.x), start, kManySetup, keys.tiles,
                                       Join{0, 0, 0, r.q.first, tile * kRows, min(r.q.count * group - tile * kRows, kRows), head, 0});
     bool first = true;
-    while (true) {
-        const Keys keys = uniform(many_keys(a, r, group, tile, kRows));
-        const int n = uniform((int)min((int64_t)(keys.tiles - t0), stop - (start + kSetup + t0))), rows = r.q.count * group;
-        if (n < 1) return;
-        const int held = r.q.held, end = keys.end, from = keys.begin + t0 * kManyKeys;
-        const int row0 = tile * kRows + 32 * kTiles * wave;  // this wave's first row
+
+    // Pages and scales of 64 pieces of 16 keys, one a lane: 16 blocks, and of the 16 behind them
+    struct Pieces {
+        int page;
+        uint32_t scales;  // bytes of K and V; bit 16: the page is there
+    };
+    Pieces pieces{-1, 0}, ahead{-1, 0};
+    int n, from;
+    const auto look_up_page = [&](Pieces &p, int i) {
+        const int k = from + i * kManyKeys + 16 * lane;
+        p.page = k < keys.end ? page_at(a.t, s, k >> shift) : -1;
+    };
+    const auto look_up_scales = [&](Pieces &p) {
+        const int64_t block = (int64_t)p.page * a.kv_heads + head;
+        p.scales = 0;
+        if (p.page >= 0) p.scales = 0x10000 | a.k_scales[block] | (uint32_t)a.v_scales[block] << 8;
+    };
+    // the run's tiles of keys of this row tile, and the first pages
+    const auto begin = [&] {
+        n = uniform((int)min((int64_t)(keys.tiles - t0), stop - (start + kManySetup + t0)));
+        from = keys.begin + t0 * kManyKeys;
+        if (n > 0) look_up_page(pieces, 0);
+    };
+    begin();
+    while (n > 0) {
+        const int held = r.q.held, end = keys.end, rows = r.q.count * group;
+        const int row0 = tile * kRows + 32 * wave, row = min(row0 + col, rows - 1);  // this wave's first row, and this lane's
         const bool active = row0 < rows;
+        const int token = token_of(a, row, group), of_group = row - token * group, position = held + token;
+        // positions of the wave's first and last row, by which its blocks are taken, masked or left out
+        const int low = __builtin_amdgcn_readfirstlane(position), high = __builtin_amdgcn_readlane(position, 31);
 
-        // Pages and scales of 64 pieces of 16 keys, one a lane: 16 blocks
-        int page = -1;
-        uint32_t scales = 0;  // bytes of K and V; bit 16: the page is there
-        const auto look_up_page = [&](int i) {
-            const int k = from + i * kManyKeys + 16 * lane;
-            page = k < end ? page_at(a.t, s, k >> shift) : -1;
+        struct Block { uint32_t scales0, scales1, scales2, scales3; };  // of its four pieces
+        const auto block_of = [&](int i) {
+            const auto of = [&](int j) { return (uint32_t)__builtin_amdgcn_readlane((int)pieces.scales, 4 * (i & 15) + j); };
+            return Block{of(0), of(1), of(2), of(3)};
         };
-        const auto look_up_scales = [&] {
-            uint32_t b0 = 0, b1 = 0;
-            if (page >= 0) b0 = a.k_scales[(int64_t)page * a.kv_heads + head], b1 = a.v_scales[(int64_t)page * a.kv_heads + head];
-            scales = b0 | b1 << 8 | (page >= 0 ? 0x10000 : 0);
-        };
-        look_up_page(0);
-
-        // this lane's queries: rows, tokens, heads of the group
-        int position[kTiles], token[kTiles], of_group[kTiles];
-        bf16x8_t q[kTiles][D / 16][kQ];
+        int to_stage = 0, stage = 0;
+        auto issue = [&](int i) {
+            // (scalar multiplications: unsigned, of 32 bits each)
+            const int p = __builtin_amdgcn_readlane(pieces.page, 4 * (i & 15) + wave);
+            const uint64_t block = ((uint64_t)(uint32_t)max(p, 0) * (uint32_t)a.kv_heads + (uint32_t)head) << shift << __builtin_ctz(D);
+            const uint32_t bytes = p < 0 ? 0 : (uint32_t)D << shift;
+            const rsrc_t in_k = make_rsrc(a.k_pages + block, bytes), in_v = make_rsrc(a.v_pages + block, bytes);
+            const uint32_t at = (uint32_t)((from + i * kManyKeys + 16 * wave) & in_page) * D;
+            char *const to = smem + to_stage + wave * 16 * D;
+            to_stage = to_stage + kStage == kManyStages * kStage ? 0 : to_stage + kStage;
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-            const int row = min(row0 + 32 * t + col, rows - 1);
-            token[t] = row / group, of_group[t] = row - token[t] * group, position[t] = held + token[t];
-            const T *in = reinterpret_cast<const T *>(a.q) + (int64_t)(r.q.first + token[t]) * a.ldq + (int64_t)(head * group + of_group[t]) * D;
+            for (int j = 0; j < kLoads / 2; ++j) issue_load_to(in_k, off_k[j], at, to + j * 1024);
+#pragma unroll
+            for (int j = 0; j < kLoads / 2; ++j) issue_load_to(in_v, off_v[j], at, to + kManyKeys * D + j * 1024);
+        };
+        issue(0), issue(1);
+        look_up_scales(pieces);
+
+        // this lane's query
+        bf16x8_t q[D / 16][kQ];
+        {
+            const T *in = reinterpret_cast<const T *>(a.q) + (int64_t)(r.q.first + token) * a.ldq + (int64_t)(head * group + of_group) * D;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {
                 Eight<T> raw;
@@ -678,70 +742,45 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
                 raw.get(v);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] *= sign;
-                split_eight(v, q[t][i]);
+                split_eight(v, q[i]);
             }
         }
-        // positions of the wave's first and last row, by which its blocks are taken, masked or left out
-        const int low = __builtin_amdgcn_readfirstlane(position[0]), high = __builtin_amdgcn_readlane(position[kTiles - 1], 31);
-        look_up_scales();
         wait_vmem<0>();
-        asm volatile("" : "+v"(page), "+v"(scales));
+        asm volatile("" : "+v"(pieces.scales));
 
-        struct Block { uint32_t scales0, scales1, scales2, scales3; };  // of its four pieces
-        int to_stage = 0, stage = 0;
-        auto issue = [&](int i) {
-            if ((i & 15) == 0 && i) {
-                look_up_page(i);
-                look_up_scales();
-                wait_vmem<0>();
-                asm volatile("" : "+v"(page), "+v"(scales));
-            }
-            const int piece = 4 * (i & 15), p = __builtin_amdgcn_readlane(page, piece + wave);
-            const rsrc_t in_k = block_rsrc(a.k_pages, a, p, head, D), in_v = block_rsrc(a.v_pages, a, p, head, D);
-            const uint32_t at = (uint32_t)((from + i * kManyKeys + 16 * wave) & in_page) * D;
-            char *const to = smem + to_stage + wave * 16 * D;
-            to_stage = to_stage + kStage == kManyStages * kStage ? 0 : to_stage + kStage;
+        float16_t o[D / 32];
 #pragma unroll
-            for (int j = 0; j < kLoads / 2; ++j) issue_load_to(in_k, off_k[j], at, to + j * 1024);
-#pragma unroll
-            for (int j = 0; j < kLoads / 2; ++j) issue_load_to(in_v, off_v[j], at, to + kManyKeys * D + j * 1024);
-            const auto of = [&](int j) { return (uint32_t)__builtin_amdgcn_readlane((int)scales, piece + j); };
-            return Block{of(0), of(1), of(2), of(3)};
-        };
-
-        float16_t o[kTiles][D / 32];
-        float m[kTiles], l[kTiles];
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-            m[t] = -INFINITY, l[t] = 0.f;
-#pragma unroll
-            for (int d = 0; d < D / 32; ++d) o[t][d] = float16_t{};
-        }
+        for (int d = 0; d < D / 32; ++d) o[d] = float16_t{};
+        float m = -INFINITY, l = 0.f;
         // A maximum that rises by more than 2^8 leaves the loop, which takes the block up again behind it: sums that are scaled on
         // one of two paths inside would be copied on the other, all of them for each block.
-        Block now = issue(0), next = issue(1), of = now;
-        const char *in = smem;
+        Block now = block_of(0), next = block_of(1), of = now;
+        int in = 0;
         bool loaded = false, there = true;
         int i = 0;
         while (i < n) {
-            float raised[kTiles];
+            float raised = -INFINITY;
             for (; i < n; ++i) {
                 const int k = from + i * kManyKeys;
                 if (!loaded) {
                     wait_vmem<kLoads>();  // this wave's part of the block has arrived, and what it read of the one before
                     wait_lds();
                     wg_barrier();
-                    of = now, now = next, next = issue(i + 2);
-                    in = smem + stage;
+                    // (the pieces of the next 16 blocks: pages, then scales, then both)
+                    if ((i & 15) == 3) look_up_page(ahead, (i & ~15) + 16);
+                    if ((i & 15) == 8) look_up_scales(ahead);
+                    if ((i & 15) == 14) pieces = ahead;
+                    issue(i + 2);
+                    of = now, now = next, next = block_of(i + 2);
+                    in = stage;
                     stage = stage + kStage == kManyStages * kStage ? 0 : stage + kStage;
                     there = (of.scales0 & of.scales1 & of.scales2 & of.scales3) >> 16;
                     if (!there || k + kManyKeys > end) {
                         // values that are not there: zeros, whatever lies in their places (a weight of zero does not cancel a NaN)
-                        for (int j = tid; j < kManyKeys * D / 16; j += 256) {
-                            const int row = j / (D / 16);
-                            const uint32_t piece = row < 32 ? (row < 16 ? of.scales0 : of.scales1) : (row < 48 ? of.scales2 : of.scales3);
-                            if (!(piece >> 16) || k + row >= end)
-                                *reinterpret_cast<uint4_t *>(const_cast<char *>(in) + kManyKeys * D + 16 * j) = uint4_t{0, 0, 0, 0};
+                        const uint32_t s0 = of.scales0, s1 = of.scales1, s2 = of.scales2, s3 = of.scales3, piece = wave < 2 ? (wave == 0 ? +s0 : +s1) : (wave == 2 ? +s2 : +s3);
+                        for (int j = lane; j < D; j += 64) {  // this wave's 16 keys, 16 bytes at a time
+                            const int key = 16 * wave + j / (D / 16);
+                            if (!(piece >> 16) || k + key >= end) *reinterpret_cast<uint4_t *>(smem + in + (kManyKeys + 16 * wave) * D + 16 * j) = uint4_t{0, 0, 0, 0};
                         }
                         wait_lds();
                         wg_barrier();
@@ -755,146 +794,148 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int j = 0; j < D / 32; ++j) raw_k[h][j] = *reinterpret_cast<const int4v_t *>(in + at_k[j] + 32 * h * D);
-                int2v_t raw_v[4][D / 32];
-#pragma unroll
-                for (int step = 0; step < 4; ++step)
-#pragma unroll
-                    for (int d = 0; d < D / 32; ++d)
-                        raw_v[step][d] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) int2v_t *)(in + at_v[d] + 16 * step * D));
-                float16_t sc[kTiles][2];
+                    for (int j = 0; j < D / 32; ++j) raw_k[h][j] = *reinterpret_cast<const int4v_t *>(smem + in + at_k[j] + 32 * h * D);
+                float16_t sc[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const float power = col < 16 ? scale_of(of_piece[2 * h] & 255) : scale_of(of_piece[2 * h + 1] & 255);
-#pragma unroll
-                    for (int t = 0; t < kTiles; ++t) sc[t][h] = float16_t{};
+                    sc[h] = float16_t{};
 #pragma unroll
                     for (int j = 0; j < D / 32; ++j)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             const bf16x8_t f = widen_eight(raw_k[h][j][2 * e], raw_k[h][j][2 * e + 1], power, power);
 #pragma unroll
-                            for (int p = kQ - 1; p >= 0; --p)
-#pragma unroll
-                                for (int t = 0; t < kTiles; ++t) sc[t][h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, q[t][2 * j + e][p], sc[t][h], 0, 0, 0);
+                            for (int p = kQ - 1; p >= 0; --p) sc[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, q[2 * j + e][p], sc[h], 0, 0, 0);
                         }
                 }
+                // (while the last products run)
+                int2v_t raw_v[D / 32][4];
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d) read_transposed<16 * D>(raw_v[d], lds_address(smem) + in + at_v[d]);
                 if (!there || k + kManyKeys - 1 > low || (a.window && k <= high - a.window)) {
+                    // keys of a lane, counted from its first, that the row sees: those above `over`, up to `upto`
+                    int upto = min(position, end - 1) - k - 4 * g, over = a.window ? position - a.window - k - 4 * g : -1;
+                    asm("" : "+v"(upto), "+v"(over));
 #pragma unroll
-                    for (int t = 0; t < kTiles; ++t)
+                    for (int h = 0; h < 2; ++h)
 #pragma unroll
-                        for (int h = 0; h < 2; ++h)
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                const int key = k + 32 * h + 8 * (e >> 2) + 4 * g + (e & 3);
-                                const bool seen = (of_piece[2 * h + (e >> 3)] >> 16) && key < end && key <= position[t] && (!a.window || key > position[t] - a.window);
-                                sc[t][h][e] = seen ? sc[t][h][e] : -INFINITY;
-                            }
+                        for (int e = 0; e < 16; ++e) {
+                            const int key = 32 * h + 8 * (e >> 2) + (e & 3);
+                            const bool seen = (of_piece[2 * h + (e >> 3)] >> 16) && key <= upto && key > over;
+                            sc[h][e] = seen ? sc[h][e] : -INFINITY;
+                        }
                 }
-                bool rises = false;
+                float top = sc[0][0];
 #pragma unroll
-                for (int t = 0; t < kTiles; ++t) {
-                    float top = sc[t][0][0];
-#pragma unroll
-                    for (int e = 1; e < 32; ++e) top = __builtin_fmaxf(top, sc[t][e >> 4][e & 15]);
-                    float t_a, t_b;
-                    swap32(top, t_a, t_b);
-                    raised[t] = __builtin_fmaxf(t_a, t_b);
-                    rises |= m[t] > -INFINITY && (raised[t] - m[t]) * c > 8.f;
+                for (int e = 1; e < 32; ++e) top = __builtin_fmaxf(top, sc[e >> 4][e & 15]);
+                float t_a, t_b;
+                swap32(top, t_a, t_b);
+                top = __builtin_fmaxf(t_a, t_b);
+                if (__ballot(m > -INFINITY && (top - m) * c > 8.f)) {
+                    raised = top;
+                    break;
                 }
-                if (__ballot(rises)) break;
-                float top_c[kTiles];
-#pragma unroll
-                for (int t = 0; t < kTiles; ++t) {
-                    m[t] = m[t] == -INFINITY ? raised[t] : m[t];  // (its sums are zeros so far)
-                    top_c[t] = m[t] == -INFINITY ? 0.f : m[t] * c;
-                }
+                m = m == -INFINITY ? top : m;  // (its sums are zeros so far)
+                const float top_c = m == -INFINITY ? 0.f : m * c;
 #pragma unroll
                 for (int step = 0; step < 4; ++step) {
-                    bf16x8_t w[kTiles][kP];
+                    float p[8];
 #pragma unroll
-                    for (int t = 0; t < kTiles; ++t) {
-                        float p[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) p[e] = weight(sc[t][step >> 1][8 * (step & 1) + e], c, top_c[t]);
-                        l[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-                        split_eight(p, w[t]);
-                    }
+                    for (int e = 0; e < 8; ++e) p[e] = weight(sc[step >> 1][8 * (step & 1) + e], c, top_c);
+                    l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+                    bf16x8_t w[kP];
+                    split_eight(p, w);
                     const float power = scale_of(of_piece[step] >> 8 & 255);
 #pragma unroll
                     for (int d = 0; d < D / 32; ++d) {
-                        const bf16x8_t f = widen_eight(raw_v[step][d][0], raw_v[step][d][1], power, power);
+                        const bf16x8_t f = widen_eight(raw_v[d][step][0], raw_v[d][step][1], power, power);
 #pragma unroll
-                        for (int e = kP - 1; e >= 0; --e)
-#pragma unroll
-                            for (int t = 0; t < kTiles; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, w[t][e], o[t][d], 0, 0, 0);
+                        for (int e = kP - 1; e >= 0; --e) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, w[e], o[d], 0, 0, 0);
                     }
                 }
             }
             if (i == n) break;
             loaded = true;
+            raised = __builtin_fmaxf(m, raised);
+            const float shrink = m == -INFINITY ? 1.f : weight(m, c, raised * c);
+            l *= shrink;
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) {
-                raised[t] = __builtin_fmaxf(m[t], raised[t]);
-                const float shrink = m[t] == -INFINITY ? 1.f : weight(m[t], c, raised[t] * c);
-                l[t] *= shrink;
+            for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-                for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) o[t][d][e] *= shrink;
-                m[t] = raised[t];
-            }
+                for (int e = 0; e < 16; ++e) o[d][e] *= shrink;
+            m = raised;
         }
+        const bool whole = n == keys.tiles;
+        const int in_tile0 = 32 * wave, last_row = rows - row0;  // (rows of the wave, if positive)
+        float *const out = whole ? nullptr : a.many_partial + (int64_t)(2 * worker + !first) * partial_floats(kRows, D);
+        const int of_first = r.q.first, of_head = head * group;
+        first = false;
+        // the next row tile that has keys, whose first pages are on their way while this one's sums are stored
+        start += kManySetup + keys.tiles, t0 = 0;
+        if (start < stop) {
+            do {
+                if (++u == units) {
+                    u = 0, s = 0;
+                    if (++head == a.kv_heads) return;  // (only where cu does not ascend)
+                    r = uniform(all.span(s));
+                }
+                while (s + 1 < sequences && uniform(start_of(s + 1)) <= u) r = uniform(all.span(++s));
+                tile = u - uniform(start_of(s));
+                keys = uniform(many_keys(a, r, group, tile, kRows));
+            } while (keys.tiles == 0);
+        }
+        begin();
         wait_vmem_and_lds<0>();
         wg_barrier();  // the stages are free
 
-        const bool whole = n == keys.tiles;
-        float *const out = whole ? nullptr : a.many_partial + (int64_t)(2 * worker + !first) * partial_floats(kRows, D);
+        // The wave's sums pass through LDS of its own, 64 elements of its 32 rows at a time, so that rows are stored in long runs
+        float l_a, l_b;
+        swap32(l, l_a, l_b);
+        l = l_a + l_b;
+        constexpr int kPitch = 68;
+        float *const staged = reinterpret_cast<float *>(smem) + wave * (32 * kPitch + 64);
+        static_assert(4 * (32 * kPitch + 64) * 4 <= many_ring<D>(), "the stages hold them");
+        if (g == 0) staged[32 * kPitch + col] = m, staged[32 * kPitch + 32 + col] = l;
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-            float l_a, l_b;
-            swap32(l[t], l_a, l_b);
-            const float sum = l_a + l_b;
-            const int in_tile = 32 * (kTiles * wave + t) + col;
-            if (row0 + 32 * t + col < rows) {
+        for (int d = 0; d < D; d += 64) {
 #pragma unroll
-                for (int d = 0; d < D / 32; ++d)
+            for (int e = 0; e < 8; ++e)
+                *reinterpret_cast<float4_t *>(staged + col * kPitch + 8 * e + 4 * g) =
+                    float4_t{o[d / 32 + e / 4][4 * (e & 3)], o[d / 32 + e / 4][4 * (e & 3) + 1], o[d / 32 + e / 4][4 * (e & 3) + 2], o[d / 32 + e / 4][4 * (e & 3) + 3]};
+            wait_lds();
+            fence();
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float4_t v = {o[t][d][4 * e], o[t][d][4 * e + 1], o[t][d][4 * e + 2], o[t][d][4 * e + 3]};
-                        const int at = 32 * d + 8 * e + 4 * g;
-                        if (whole)
-                            finish<T>(a, r.q.first + token[t], head * group + of_group[t], at, D, v, m[t], sum);
-                        else
-                            *reinterpret_cast<float4_t *>(out + in_tile * D + at) = v;
+            for (int j = 0; j < 4; ++j) {
+                const int of = 8 * j + (lane >> 3), at = 8 * (lane & 7);
+                const float4_t lo = *reinterpret_cast<const float4_t *>(staged + of * kPitch + at), hi = *reinterpret_cast<const float4_t *>(staged + of * kPitch + at + 4);
+                const float top = staged[32 * kPitch + of], sum = staged[32 * kPitch + 32 + of];
+                if (of < last_row) {
+                    if (whole) {
+                        const int token = token_of(a, row0 + of, group);
+                        finish_eight<T>(a, of_first + token, of_head + row0 + of - token * group, d + at, D, lo, hi, top, sum);
+                    } else {
+                        float *const to = out + (in_tile0 + of) * D + d + at;
+                        *reinterpret_cast<float4_t *>(to) = lo, *reinterpret_cast<float4_t *>(to + 4) = hi;
+                        if (d + at == 0) out[kRows * D + in_tile0 + of] = top, out[kRows * (D + 1) + in_tile0 + of] = sum;
                     }
-                if (!whole && g == 0) out[kRows * D + in_tile] = m[t], out[kRows * (D + 1) + in_tile] = sum;
+                }
             }
+            wait_lds();
+            fence();
         }
-        first = false;
-        start += kSetup + keys.tiles, t0 = 0;
-        if (start >= stop) break;
-        // the next row tile that has keys
-        do {
-            if (++u == units) {
-                u = 0, s = 0;
-                if (++head == a.kv_heads) return;  // (only where cu does not ascend)
-                r = uniform(all.span(s));
-            }
-            while (s + 1 < sequences && uniform(start_of(s + 1)) <= u) r = uniform(all.span(++s));
-            tile = u - uniform(start_of(s));
-        } while (uniform(many_keys(a, r, group, tile, kRows)).tiles == 0);
+        wg_barrier();  // before the next row tile's keys come
     }
 }
 
 // ---- both ----------------------------------------------------------------------------------------------------------------------
-// Joins what several workgroups have left of one tile of rows, in their order, the largest maximum first: a workgroup for each
-// beginning of a run and kRows rows.  What few workgroups left is added by the threads of a row; of more, all teams of D / 4
-// lanes take a share.
+// Joins what several workgroups have left of one tile of rows, in their order, the largest maximum first: for each beginning of
+// a run as many workgroups as the grid's other dimension has, which deal out its rows.  What few workgroups left is added by the
+// D / 4 lanes of a row; of more, all teams of so many take a share.
 template <int D, typename T, bool MANY>
 __global__ __launch_bounds__(256) void cache_attention_join_kernel(const AttentionArgs a)
 {
-    constexpr int kRows = MANY ? 8 : 1, kTile = MANY ? many_rows<D>() : kFewRows, kWorkers = MANY ? many_workers<D, T>() : few_workers<D>();
+    constexpr int kTile = MANY ? kManyRows : kFewRows, kWorkers = MANY ? many_workers<D, T>() : few_workers<D>();
     constexpr int kLanes = D / 4, kTeams = 256 / kLanes, kSerial = 8;
     __shared__ float factor[kWorkers], of_wave[2][4];
     __shared__ float4_t sums[kTeams][kLanes];
@@ -907,11 +948,11 @@ __global__ __launch_bounds__(256) void cache_attention_join_kernel(const Attenti
     const float c = log2_scale(a);
     const int d = tid % kLanes, team = tid / kLanes;
     const auto put = [&](int row, float4_t v, float top, float sum) {
-        const int of_all = j.row0 + row, token = of_all / group;
+        const int of_all = j.row0 + row, token = token_of(a, of_all, group);
         finish<T>(a, j.first + token, j.head * group + of_all - token * group, 4 * d, D, v, top, sum);
     };
     if (count <= kSerial) {
-        for (int row = blockIdx.y * kRows + team; row < min((int)(blockIdx.y + 1) * kRows, rows); row += kTeams) {
+        for (int row = blockIdx.y * kTeams + team; row < rows; row += gridDim.y * kTeams) {
             float m[kSerial], l[kSerial], top = -INFINITY, sum = 0.f;
             float4_t o[kSerial];
 #pragma unroll
@@ -932,7 +973,7 @@ __global__ __launch_bounds__(256) void cache_attention_join_kernel(const Attenti
         }
         return;
     }
-    for (int row = blockIdx.y * kRows; row < min((int)(blockIdx.y + 1) * kRows, rows); ++row) {
+    for (int row = blockIdx.y; row < rows; row += gridDim.y) {
         float top = -INFINITY;
         for (int i = tid; i < count; i += 256) {
             factor[i] = partial(i)[kTile * D + row];
@@ -977,26 +1018,28 @@ static Scratch scratch(int64_t tokens, int64_t max_tokens, int64_t group)
     s.many_join = few_workers<D>() * sizeof(Join);
     s.few_partial = s.many_join + kMany * sizeof(Join);
     s.many_partial = s.few_partial + 8ll * few_workers<D>() * partial_floats(kFewRows, D);
-    s.bytes = s.many_partial + (many ? 8ll * kMany * partial_floats(many_rows<D>(), D) : 0);
+    s.bytes = s.many_partial + (many ? 8ll * kMany * partial_floats(kManyRows, D) : 0);
     return s;
 }
 
 template <int D, typename T>
 static perf_status attention(AttentionArgs &a, char *workspace, hipStream_t st)
 {
-    const int64_t group = a.q_heads / a.kv_heads, units = many_units(a.t.tokens, a.t.sequences, group, many_rows<D>());
-    if (units > INT32_MAX) return PERF_ERR_UNSUPPORTED;
+    const int64_t group = a.q_heads / a.kv_heads, units = many_units(a.t.tokens, a.t.sequences, group, kManyRows);
+    if (a.t.tokens * group > kMaxExtent8) return PERF_ERR_UNSUPPORTED;  // (rows of a sequence are counted in 31 bits)
+    a.group_magic = div_magic(group);
     const Scratch at = scratch<D>(a.t.tokens, a.max_tokens, group);
     a.few_join = (Join *)workspace, a.many_join = (Join *)(workspace + at.many_join);
     a.few_partial = (float *)(workspace + at.few_partial), a.many_partial = (float *)(workspace + at.many_partial);
     const bool many = a.max_tokens * group > kFewRows;  // (whether a sequence of as many tokens is for the other kernel)
     if (!allow_lds<cache_attention_few_kernel<D, T>>(few_lds<D>())) return PERF_ERR_LAUNCH;
     cache_attention_few_kernel<D, T><<<few_workers<D>(), 256, few_lds<D>(), st>>>(a);
-    cache_attention_join_kernel<D, T, false><<<dim3(few_workers<D>(), (uint32_t)std::min<int64_t>(kFewRows, a.max_tokens * group)), 256, 0, st>>>(a);
+    const uint32_t rows = (uint32_t)std::min<int64_t>(kFewRows, a.max_tokens * group);
+    cache_attention_join_kernel<D, T, false><<<dim3(few_workers<D>(), rows), 256, 0, st>>>(a);
     if (many) {
         if (!allow_lds<cache_attention_many_kernel<D, T>>(many_lds<D>())) return PERF_ERR_LAUNCH;
         cache_attention_many_kernel<D, T><<<many_workers<D, T>(), 256, many_lds<D>(), st>>>(a, (int)units);
-        cache_attention_join_kernel<D, T, true><<<dim3(many_workers<D, T>(), many_rows<D>() / 8), 256, 0, st>>>(a);
+        cache_attention_join_kernel<D, T, true><<<dim3(many_workers<D, T>(), 16), 256, 0, st>>>(a);
     }
     return launch_status();
 }
