@@ -31,6 +31,12 @@ struct Join {
     int unused;
 };
 
+// lse: -infinity without keys, whose maximum is -infinity, for a scale of 0 too
+__device__ __forceinline__ float log_of_sum(const AttentionArgs &a, float top, float sum)
+{
+    return sum == 0.f ? -INFINITY : __builtin_fmaf(top, fabsf(a.scale), logf(sum));
+}
+
 // Elements d .. d + 3 of a query and head from the sums of weights and of weighted values
 template <typename T>
 __device__ __forceinline__ void finish(const AttentionArgs &a, int token, int head, int d, int D, float4_t v, float top, float sum)
@@ -39,7 +45,7 @@ __device__ __forceinline__ void finish(const AttentionArgs &a, int token, int he
     T *const o = reinterpret_cast<T *>(a.o) + (int64_t)token * a.ldo + (int64_t)head * D + d;
     const float w[4] = {v[0] * r, v[1] * r, v[2] * r, v[3] * r};
     store_row_chunk<true, T, 4>(o, w);
-    if (a.lse && d == 0) a.lse[(int64_t)token * a.q_heads + head] = __builtin_fmaf(top, fabsf(a.scale), logf(sum));
+    if (a.lse && d == 0) a.lse[(int64_t)token * a.q_heads + head] = log_of_sum(a, top, sum);
 }
 
 template <typename T>
@@ -48,7 +54,7 @@ __device__ __forceinline__ void finish_eight(const AttentionArgs &a, int token, 
     const float r = sum == 0.f ? 0.f : 1.0f / sum;
     const float w[8] = {lo[0] * r, lo[1] * r, lo[2] * r, lo[3] * r, hi[0] * r, hi[1] * r, hi[2] * r, hi[3] * r};
     store_row_chunk<true, T, 8>(reinterpret_cast<T *>(a.o) + (int64_t)token * a.ldo + (int64_t)head * D + d, w);
-    if (a.lse && d == 0) a.lse[(int64_t)token * a.q_heads + head] = __builtin_fmaf(top, fabsf(a.scale), logf(sum));
+    if (a.lse && d == 0) a.lse[(int64_t)token * a.q_heads + head] = log_of_sum(a, top, sum);
 }
 
 __device__ __forceinline__ int token_of(const AttentionArgs &a, int row, int group) { return div_by(row, group, a.group_magic); }
@@ -535,8 +541,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
         if (start < stop) {
             if (++head == a.kv_heads) {
                 head = 0;
-                do r = uniform(sequences.span(++s)), tiles = few_tiles(a, r);
-                while (tiles == 0);
+                do {
+                    if (++s >= a.t.sequences) return;  // (there is one, unless the lengths change meanwhile)
+                    r = uniform(sequences.span(s)), tiles = few_tiles(a, r);
+                } while (tiles == 0);
             }
         }
         begin();
