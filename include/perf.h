@@ -361,9 +361,10 @@ perf_status perf_cache_append_fp8(const void *q, const void *k, const void *v, c
  * query i of sequence s, at position p = lengths[s] + i, and head h, which reads head h / (q_heads/kv_heads) of the cache, over
  * the keys j <= p, with a window only those > p - window, whose page is there:
  *     S_j = scale * q . k_j,   o = sum_j exp(S_j) v_j / sum_j exp(S_j),   lse = log sum_j exp(S_j)   (natural logarithm).
- * Scores, exponentials and sums are fp32, o is rounded once.  bf16 queries: the weights exp(S_j - max) are rounded to bf16 for
- * their product with the values (2^-8 of each at most; their sum is taken before).  fp32 queries and weights are split into three bf16, so
- * that every product counts to 2^-24.  A query that sees no key gets o = 0 and lse = -infinity.
+ * Scores, exponentials and sums are fp32, o is rounded once.  bf16 queries: the weights exp(S_j - max) are rounded for their
+ * product with the values, by 2^-8 of each at most (2^-16 in sequences that bring few tokens: up to 16 queries to a head of the
+ * cache); their sum is taken before.  fp32 queries and weights are split into three bf16, so that every product counts to 2^-24.
+ * A query that sees no key gets o = 0 and lse = -infinity.
  *   q, o       device, tokens x q_heads*head_dim, row strides ldq and ldo, x_dt
  *   lse        device fp32, tokens x q_heads, rows close; or NULL
  *   workspace  device, at least perf_cache_attention_fp8_workspace_bytes(...) bytes of the same arguments, 16-byte aligned,
@@ -373,7 +374,7 @@ perf_status perf_cache_append_fp8(const void *q, const void *k, const void *v, c
  * What one block of scale 255 holds may turn every query of its sequence in the call to NaN.
  * The workspace's size is -1 for arguments that the call would reject.
  * Errors: NULL (all but lse), SHAPE (as perf_cache_append_fp8; max_tokens < 1, window < 0 or > 2^30, scale not finite), DTYPE,
- * ALIGN, UNSUPPORTED (head_dim or page_size as above, more work than a launch holds), LAUNCH. */
+ * ALIGN, UNSUPPORTED (head_dim or page_size as above, tokens * (q_heads/kv_heads) > 2^30), LAUNCH. */
 int64_t perf_cache_attention_fp8_workspace_bytes(int64_t tokens, int64_t sequences, int64_t max_tokens, int64_t q_heads,
                                                  int64_t kv_heads, int64_t head_dim, int64_t page_size, int64_t table_pages);
 perf_status perf_cache_attention_fp8(const void *q, const void *k_pages, const void *v_pages, const uint8_t *k_scales,

@@ -206,7 +206,7 @@ __device__ __forceinline__ Place find_place(PlaceScratch &at, int items, int cop
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int each = (items + 255) / 256, from = min(tid * each, items), to = min(from + each, items);
     int64_t mine = 0;
-    tiles_of(from, to, [&](int, int n) { mine += n; });
+    tiles_of(from, to, [&](int, int64_t n) { mine += n; });
     int64_t upto = mine;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -231,7 +231,7 @@ __device__ __forceinline__ Place find_place(PlaceScratch &at, int items, int cop
     const int64_t x = p.start - p.copy * one;
     int64_t before = upto - mine;
     if (some && x >= before && x < upto)
-        tiles_of(from, to, [&](int i, int n) {
+        tiles_of(from, to, [&](int i, int64_t n) {
             if (x >= before && x < before + n) at.before = before, at.item = i;
             before += n;
         });
@@ -253,7 +253,8 @@ __device__ __forceinline__ Join join_at(const Place &p, int worker, int workers,
     j.count = 0, j.from = worker - 1, j.odd = 0, j.unused = 0;
     const int64_t before = worker ? run_start(p.total, worker - 1, workers) : 0, first = start + setup;
     if (worker && first < p.start && first >= before) {
-        j.count = worker_of(p.total, first + tiles - 1, workers) - j.from + 1;
+        // (the last of them at most: where cu does not ascend, tiles may be other ones than those counted)
+        j.count = min(worker_of(p.total, first + tiles - 1, workers), workers - 1) - j.from + 1;
         j.odd = before < start;
     }
     return j;
@@ -320,7 +321,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
     const Place place = find_place(*reinterpret_cast<PlaceScratch *>(smem), a.t.sequences, 1, worker, gridDim.x, [&](int i, int to, auto &&take) {
         for (; i < to; ++i) {
             const int tiles = few_tiles(a, sequences.span(i));
-            take(i, tiles ? (kFewSetup + tiles) * a.kv_heads : 0);
+            take(i, tiles ? (int64_t)(kFewSetup + tiles) * a.kv_heads : 0);
         }
     });
     const int64_t stop = place.stop;
@@ -1034,7 +1035,6 @@ template <int D, typename T>
 static perf_status attention(AttentionArgs &a, char *workspace, hipStream_t st)
 {
     const int64_t group = a.q_heads / a.kv_heads, units = many_units(a.t.tokens, a.t.sequences, group, kManyRows);
-    if (a.t.tokens * group > kMaxExtent8) return PERF_ERR_UNSUPPORTED;  // (rows of a sequence are counted in 31 bits)
     a.group_magic = div_magic(group);
     const Scratch at = scratch<D>(a.t.tokens, a.max_tokens, group);
     a.few_join = (Join *)workspace, a.many_join = (Join *)(workspace + at.many_join);
@@ -1061,11 +1061,14 @@ static bool attention_shape_ok(const CacheShape &c, int64_t max_tokens)
     return cache_shape_ok(c) && c.head_dim <= kMaxExtent8 / kMaxHeads && max_tokens >= 1;
 }
 
+// (rows of a sequence are counted in 31 bits)
+static bool attention_supported(const CacheShape &c) { return cache_supported(c) && c.tokens * (c.q_heads / c.kv_heads) <= kMaxExtent8; }
+
 extern "C" int64_t perf_cache_attention_fp8_workspace_bytes(int64_t tokens, int64_t sequences, int64_t max_tokens, int64_t q_heads,
                                                             int64_t kv_heads, int64_t head_dim, int64_t page_size, int64_t table_pages)
 {
     const CacheShape c{tokens, sequences, q_heads, kv_heads, head_dim, 1, page_size, table_pages, table_pages};
-    if (!attention_shape_ok(c, max_tokens) || !cache_supported(c)) return -1;
+    if (!attention_shape_ok(c, max_tokens) || !attention_supported(c)) return -1;
     const int64_t group = q_heads / kv_heads;
     return (head_dim == 64    ? scratch<64>(tokens, max_tokens, group)
             : head_dim == 128 ? scratch<128>(tokens, max_tokens, group)
@@ -1090,7 +1093,7 @@ extern "C" perf_status perf_cache_attention_fp8(const void *q, const void *k_pag
     if (!aligned(q, size) || !aligned(o, size) || !aligned(lse, 4) || !aligned(workspace, 16) || !aligned(k_pages, 16) ||
         !aligned(v_pages, 16) || !aligned(table, 4) || !aligned(lengths, 4) || !aligned(cu, 4))
         return PERF_ERR_ALIGN;
-    if (!cache_supported(c)) return PERF_ERR_UNSUPPORTED;
+    if (!attention_supported(c)) return PERF_ERR_UNSUPPORTED;
     AttentionArgs a{};
     a.t = PageTable{table, lengths, cu, ldt, (int)tokens, (int)sequences, (int)pages, (int)table_pages, __builtin_ctzll(page_size)};
     a.q = q, a.o = o, a.lse = lse, a.ldq = ldq, a.ldo = ldo;

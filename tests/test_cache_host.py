@@ -72,6 +72,15 @@ def test_workspace_size_goes_by_the_same_rules():
             assert size(**{**base, **{k: v for k, v in changes.items() if k in base}}) == -1, changes
 
 
+def test_attention_refuses_more_rows_than_it_counts():
+    wide = dict(q_heads=1024, kv_heads=1, ldq=1 << 16, ldo=1 << 16)
+    sizes = ("tokens", "sequences", "max_tokens", "q_heads", "kv_heads", "head_dim", "page_size", "table_pages")
+    big = {**ATTENTION, **wide, "tokens": (1 << 20) + 1}
+    assert perf.perf_cache_attention_fp8(**big, check=False) == UNSUPPORTED
+    assert perf.perf_cache_attention_fp8_workspace_bytes(**{k: big[k] for k in sizes}) == -1
+    assert perf.perf_cache_attention_fp8_workspace_bytes(**{k: {**big, "tokens": 1 << 20}[k] for k in sizes}) > 0
+
+
 @pytest.fixture(scope="module")
 def recorder(tmp_path_factory):
     return L.build_recorder(str(tmp_path_factory.mktemp("recorder")))

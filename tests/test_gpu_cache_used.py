@@ -180,6 +180,33 @@ def test_scale_of_zero_where_no_key_is_seen(new):
         C.assert_attention_close(*call.results(), C.attention_ref(cache, batch, q, window, 0.0), BF16, 64, 80)
 
 
+@pytest.mark.parametrize("dt", [BF16, F32])
+def test_rows_that_do_not_ascend_stay_inside(dt):
+    """Which rows are computed where cu descends is not specified; nothing is read or written outside, and the next call is right."""
+    held, new = [2000, 90, 700, 0, 300], [60, 1, 40, 9, 130]
+    batch = C.Batch(held, new, 16, 1)
+    cache = C.Cache(batch.pages, 2, 16, 64)
+    C.fill(cache, batch, 2)
+    cache.to_gpu()
+    batch.to_gpu()
+    q = C.random_queries(batch, 8, 64, dt, 3)
+    cu, n, x = batch.dev[2], batch.tokens, q[:, :2].contiguous().cuda()
+    call = C.Attention(cache, batch, q, 0, 0.125, dt)
+    for bad in ([0, n, 10, n, 20, n], [n, n - 1, 100, 50, 7, 0], [0, 200, 100, n, n - 60, n], [30, 20, 150, 140, n, 1], [-5, 2 ** 30, -2 ** 31, 2 ** 31 - 1, 5, n]):
+        cu.copy_(torch.tensor(bad, dtype=torch.int32))
+        call.run()
+        call.results()
+    cu.copy_(batch.cu)
+    call.run()
+    C.assert_attention_close(*call.results(), C.attention_ref(cache, batch, q, 0, 0.125), dt, 64, 2100)
+    for bad in ([0, n, 10, n, 20, n], [n, n - 1, 100, 50, 7, 0], [-5, 2 ** 30, -2 ** 31, 2 ** 31 - 1, 5, n]):
+        cu.copy_(torch.tensor(bad, dtype=torch.int32))
+        pages = [cache.gpu[name].data_ptr() for name in ("k", "v", "ks", "vs")]
+        perf.perf_cache_append_fp8(None, x.data_ptr(), x.data_ptr(), None, None, *pages, *batch.addresses(), n, 5, 2, 2, 64, 128, 128, 128, 128,
+                                   cache.pages, 16, batch.columns, batch.table.shape[1], 0, 0, 0, dt, stream=G.stream())
+        torch.cuda.synchronize()
+
+
 @pytest.mark.parametrize("held", [20, 0])
 def test_rows_beyond_32_bits(held):
     """Rows of tokens 2^31 elements apart."""
