@@ -2,6 +2,11 @@
 // position p = lengths[s] + i, and head h, over the keys j <= p (with a window: j > p - window) whose page the table has:
 //     S_j = scale * q . k_j,   m = max S_j,   l = sum exp(S_j - m),   o = sum exp(S_j - m) v_j / l,   lse = m + log l.
 // A query without keys gets o = 0 and lse = -inf.
+//
+// Two pairs of kernels, by the rows that a sequence brings to a head of the cache (new tokens x queries that share the head): up to
+// 16, or more; each pair takes its sequences from the whole batch, on the device, so that nothing of the lengths is needed on the
+// host.  max_tokens leaves the second pair out where no sequence can be for it; the first pair takes 4.7 + 4.6 us where none is
+// (reading the lengths, and idle workgroups).
 #include "cache.h"
 #include "fp8.h"
 #include "mfma_tile.h"
@@ -287,7 +292,13 @@ struct Sequences {
 // Decoding: bound by the bytes of the cache.  The keys of all sequences and heads, in tiles of 128, are one list that is cut into
 // equal runs, a workgroup each, whatever the lengths are; a run that begins or ends inside a head's keys leaves its sums in the
 // workspace, and the second kernel joins them in order.  Inside a workgroup each of four waves takes 32 keys of a tile through LDS
-// of its own, loaded kStages - 1 blocks ahead; they meet where a head ends.
+// of its own, kStages blocks at a time on their way: a block goes to registers whole before the next one of its stage is asked for.
+// The waves meet where a head ends.  Sequences' rows and lengths lie in LDS, of up to 512: walking from one to the next then costs
+// no trip to memory.
+//
+// 64 sequences of 64 to 32768 tokens, 8 heads of 128, 32 queries: 134 us, 5.4 TB/s (a copy of 1 GiB reaches 6.4); one of 131071
+// tokens 55 us, 5.1 TB/s; 16 of 2048 to 6000 tokens 29-31 us, 4.1 TB/s, the beginning (4.7 us: lengths, then pages, then keys) and
+// the waits where heads end being the rest.
 //
 // S^T = K Q^T and o^T = V^T P^T on v_mfma_f32_16x16x32_bf16, queries in the columns: a lane has one query, keys 4 g .. 4 g + 3 of
 // both halves of the 32 (g = lane / 16), whose weights are its share of the second product's operand as they are.  The rows of V
@@ -579,10 +590,15 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
 }
 
 // ---- many rows --------------------------------------------------------------------------------------------------------------
-// Prompts: bound by the matrix units and by the vector work beside them.  Tiles of 256 rows (128 for heads of 256) of (token, head of a group) and one
-// head of the cache meet its keys 64 at a time, which pass through three stages of LDS, loaded by all four waves, one barrier to a
-// block; each wave has 64 of the rows (32).  The blocks of all row tiles and heads are one list, cut into equal runs as above, heads first: an
+// Prompts: bound by the matrix units and by the vector work beside them.  Tiles of 128 rows of (token, head of a group) and one head
+// of the cache meet its keys 64 at a time, which pass through three stages of LDS, loaded by all four waves, one barrier to a block;
+// each wave has 32 of the rows.  The blocks of all row tiles and heads are one list, cut into equal runs as above, heads first: an
 // XCD's workgroups take neighbouring runs, which share keys in its L2.
+//
+// 4 prompts of about 2048 tokens, 8 heads of 128, 32 queries: 225-230 us, 0.6 PFLOP/s of what is seen (a large library product in
+// bf16: 1.2).  Beside the 32 products of a wave and block (0.48 us) stand some 320 vector instructions for widening keys and values,
+// exponentials and maxima, which two waves of a SIMD hide from each other in part: 1.65 us a block and SIMD.  64 rows to a wave, which
+// widens half as often, leave one wave to a SIMD: 334 us.  Keys widened once for two waves, weights through LDS: 240 us.
 //
 // The products are those above on v_mfma_f32_32x32x16_bf16: a lane has one query, and keys 4 g .. 4 g + 3 of every eight (g =
 // lane / 32).  The weights of bf16 queries are rounded to bf16 once (the few rows' kernel, which waits for memory, keeps 16 bits
@@ -940,7 +956,9 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
 // ---- both ----------------------------------------------------------------------------------------------------------------------
 // Joins what several workgroups have left of one tile of rows, in their order, the largest maximum first: for each beginning of
 // a run as many workgroups as the grid's other dimension has, which deal out its rows.  What few workgroups left is added by the
-// D / 4 lanes of a row; of more, all teams of so many take a share.
+// D / 4 lanes of a row; of more, all teams of so many take a share.  Bound by trips to memory for few rows (3.3-5 us) and by the sums'
+// bytes for many: 51 MB in 17-18 us after 4 prompts of about 2048 tokens.  (A fourth of the workgroups for few rows, where most are
+// idle, 1.7 for 4.6 us, makes a mixed batch's join 10.6 for 5.7 us.)
 template <int D, typename T, bool MANY>
 __global__ __launch_bounds__(256) void cache_attention_join_kernel(const AttentionArgs a)
 {
