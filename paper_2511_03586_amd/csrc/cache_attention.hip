@@ -192,10 +192,46 @@ __device__ __forceinline__ Span uniform(Span r)
 }
 
 // A kernel's tiles, of all items one after the other, are cut into one run for each worker, and none is empty: as many workers as
-// tiles, if those are fewer.  The worker of a tile is the last whose run begins at it or before.
-__device__ __forceinline__ int workers_of(int64_t total, int workers) { return (int)min(total, (int64_t)workers); }
-__device__ __forceinline__ int64_t run_start(int64_t total, int worker, int workers) { return total * worker / workers; }
-__device__ __forceinline__ int worker_of(int64_t total, int64_t tile, int workers) { return (int)(((tile + 1) * workers - 1) / total); }
+// tiles, if those are fewer.  Runs are equal, or, of a list that is long enough, by the Shares of the workers: of each XCD's, those
+// of the first round of workgroups (32 of them, one to a CU), of the second, of the third.
+template <int... kOfRound>
+struct Shares {
+    static constexpr int kRounds = sizeof...(kOfRound), kOf[kRounds] = {kOfRound...}, kOfXcd = 32 * (kOfRound + ...), kAll = 8 * kOfXcd;
+    // shares of the workers before this one; the worker that has this share
+    static __device__ __forceinline__ int before(int worker)
+    {
+        int xcd = worker / (32 * kRounds), at = worker - xcd * 32 * kRounds, sum = xcd * kOfXcd;
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) sum += kOf[r] * min(max(at - 32 * r, 0), 32);
+        return sum;
+    }
+    static __device__ __forceinline__ int worker(int share)
+    {
+        int xcd = share / kOfXcd, at = share - xcd * kOfXcd, found = xcd * 32 * kRounds;
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            found += min(at, 32 * kOf[r] - (r + 1 < kRounds ? 0 : 1)) / kOf[r];
+            at = max(at - 32 * kOf[r], 0);
+        }
+        return found;
+    }
+};
+template <typename S>
+struct Runs {
+    int64_t total;
+    int workers;
+    bool by_shares;
+    __device__ __forceinline__ Runs(int64_t tiles, int most) : total(tiles), workers((int)min(tiles, (int64_t)most)), by_shares(S::kRounds > 1 && tiles >= 2 * S::kAll) {}
+    __device__ __forceinline__ int64_t start(int worker) const
+    {
+        return by_shares ? total * S::before(worker) / S::kAll : total * worker / workers;
+    }
+    // the worker of a tile: the last whose run begins at it or before
+    __device__ __forceinline__ int worker(int64_t tile) const
+    {
+        return by_shares ? S::worker((int)(((tile + 1) * S::kAll - 1) / total)) : (int)(((tile + 1) * workers - 1) / total);
+    }
+};
 
 // Tiles of each of `items` (each thread adds up a run of them) and of all, `copies` times over.  The item in which the run of
 // `worker` begins and the tiles before it are found on the way.
@@ -205,7 +241,7 @@ struct Place {
     int copy, item;
 };
 struct PlaceScratch { int64_t of_wave[4], before, item; };
-template <typename Tiles>
+template <typename S, typename Tiles>
 __device__ __forceinline__ Place find_place(PlaceScratch &at, int items, int copies, int worker, int most, Tiles &&tiles_of)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -228,10 +264,10 @@ __device__ __forceinline__ Place find_place(PlaceScratch &at, int items, int cop
     }
     Place p;
     p.total = one * copies;
-    const int workers = workers_of(p.total, most);
-    const bool some = worker < workers;
-    p.start = some ? run_start(p.total, worker, workers) : 0;
-    p.stop = some ? run_start(p.total, worker + 1, workers) : 0;
+    const Runs<S> runs(p.total, most);
+    const bool some = worker < runs.workers;
+    p.start = some ? runs.start(worker) : 0;
+    p.stop = some ? runs.start(worker + 1) : 0;
     p.copy = some ? (int)(p.start / one) : 0;
     const int64_t x = p.start - p.copy * one;
     int64_t before = upto - mine;
@@ -253,13 +289,14 @@ __device__ __forceinline__ Place find_place(PlaceScratch &at, int items, int cop
 constexpr int kFewSetup = 3, kManySetup = 5;
 
 // What has to be joined where the run of `worker` begins, in a tile of rows whose places, `setup` and `tiles`, begin with `start`
-__device__ __forceinline__ Join join_at(const Place &p, int worker, int workers, int64_t start, int setup, int tiles, Join j)
+template <typename S>
+__device__ __forceinline__ Join join_at(const Place &p, const Runs<S> &runs, int worker, int64_t start, int setup, int tiles, Join j)
 {
     j.count = 0, j.from = worker - 1, j.odd = 0, j.unused = 0;
-    const int64_t before = worker ? run_start(p.total, worker - 1, workers) : 0, first = start + setup;
+    const int64_t before = worker ? runs.start(worker - 1) : 0, first = start + setup;
     if (worker && first < p.start && first >= before) {
         // (the last of them at most: where cu does not ascend, tiles may be other ones than those counted)
-        j.count = min(worker_of(p.total, first + tiles - 1, workers), workers - 1) - j.from + 1;
+        j.count = min(runs.worker(first + tiles - 1), runs.workers - 1) - j.from + 1;
         j.odd = before < start;
     }
     return j;
@@ -309,6 +346,7 @@ template <int D> constexpr int few_stages() { return D == 64 ? 4 : 2; }
 template <int D> constexpr int few_ring() { return kFewWaves * few_stages<D>() * 64 * D; }
 template <int D> constexpr int few_lds() { return few_ring<D>() + kSequencesBytes; }
 template <int D> constexpr int few_workers() { return D == 256 ? 256 : 512; }  // as many as are on the chip at a time
+using FewShares = Shares<1>;
 constexpr int partial_floats(int rows, int D) { return rows * (D + 2); }  // sums of a tile of rows, maxima, sums of weights
 
 __device__ __forceinline__ bool is_few(const AttentionArgs &a, int count) { return count * (int64_t)(a.q_heads / a.kv_heads) <= kFewRows; }
@@ -329,7 +367,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, col = lane & 15;
     const int worker = blockIdx.x, group = uniform(a.q_heads / a.kv_heads), shift = a.t.page_shift, in_page = (1 << shift) - 1;
     const Sequences sequences(a, smem + few_ring<D>());
-    const Place place = find_place(*reinterpret_cast<PlaceScratch *>(smem), a.t.sequences, 1, worker, gridDim.x, [&](int i, int to, auto &&take) {
+    const Place place = find_place<FewShares>(*reinterpret_cast<PlaceScratch *>(smem), a.t.sequences, 1, worker, gridDim.x, [&](int i, int to, auto &&take) {
         for (; i < to; ++i) {
             const int tiles = few_tiles(a, sequences.span(i));
             take(i, tiles ? (int64_t)(kFewSetup + tiles) * a.kv_heads : 0);
@@ -368,7 +406,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
     int64_t start = place.before + (int64_t)head * (kFewSetup + tiles);  // of the head's places
     int t0 = uniform((int)max(place.start - start - kFewSetup, (int64_t)0));
     if (tid == 0)
-        a.few_join[worker] = join_at(place, worker, workers_of(place.total, gridDim.x), start, kFewSetup, tiles, Join{0, 0, 0, r.q.first, 0, r.q.count * group, head, 0});
+        a.few_join[worker] = join_at(place, Runs<FewShares>(place.total, gridDim.x), worker, start, kFewSetup, tiles, Join{0, 0, 0, r.q.first, 0, r.q.count * group, head, 0});
     bool first = true;
 
     // Pages and scales of 64 blocks, one a lane: those of block i are in lane i % 64
@@ -595,9 +633,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
 // each wave has 32 of the rows.  The blocks of all row tiles and heads are one list, cut into equal runs as above, heads first: an
 // XCD's workgroups take neighbouring runs, which share keys in its L2.
 //
-// 4 prompts of about 2048 tokens, 8 heads of 128, 32 queries: 225-230 us, 0.6 PFLOP/s of what is seen (a large library product in
+// 4 prompts of about 2048 tokens, 8 heads of 128, 32 queries: 212-221 us, 0.65 PFLOP/s of what is seen (a large library product in
 // bf16: 1.2).  Beside the 32 products of a wave and block (0.48 us) stand some 320 vector instructions for widening keys and values,
-// exponentials and maxima, which two waves of a SIMD hide from each other in part: 1.65 us a block and SIMD.  64 rows to a wave, which
+// exponentials and maxima, which two waves of a SIMD hide from each other in part: 0.84 us a block and SIMD where
+// contexts are long, and beginnings and ends of row tiles, five to a workgroup, take as long again as their blocks here.  64 rows to a wave, which
 // widens half as often, leave one wave to a SIMD: 334 us.  Keys widened once for two waves, weights through LDS: 240 us.
 //
 // The products are those above on v_mfma_f32_32x32x16_bf16: a lane has one query, and keys 4 g .. 4 g + 3 of every eight (g =
@@ -608,6 +647,13 @@ constexpr int kManyKeys = 64, kManyStages = 3;
 constexpr int kManyRows = 128;
 // workgroups to a CU, by the registers that a wave needs for its queries and sums
 template <int D, typename T> constexpr int many_per_cu() { return D == 256 || (D == 128 && sizeof(T) == 4) ? 1 : D == 64 && sizeof(T) == 2 ? 3 : 2; }
+// Of workgroups that share a CU the one that came first is served first: with equal runs it ended after 167 us and the second after
+// 217 (4 prompts of about 2048 tokens, heads of 128), and the second's waves, then alone, hide nothing.  With these shares 228-235
+// us became 212-221 for the kernel, 137 -> 130 for 20 mixed ones, and with three to a CU (32 x 512, heads of 64) 67 -> 60; 6 : 5 and 3 : 2
+// are slower.  Contexts of some thousand tokens under each prompt lose 2 % (790 -> 805 us for 4 x 2048 on 4096).  The kernel for few
+// rows, which waits for memory, gains nothing by it.
+template <int D, typename T>
+using ManyShares = std::conditional_t<many_per_cu<D, T>() == 1, Shares<1>, std::conditional_t<many_per_cu<D, T>() == 2, Shares<4, 3>, Shares<7, 4, 3>>>;
 template <int D, typename T> constexpr int many_workers() { return 256 * many_per_cu<D, T>(); }
 // (three stages; for heads of 64 a little more, which the sums need on their way out)
 template <int D> constexpr int many_ring() { return std::max(kManyStages * 2 * kManyKeys * D, 4 * (32 * 68 + 64) * 4); }
@@ -652,7 +698,7 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
 
     const Sequences all(a, smem + many_ring<D>());
     const auto start_of = [&](int s) { return many_start(all.first(s), group, kRows, s); };
-    const Place place = find_place(*reinterpret_cast<PlaceScratch *>(smem), units, a.kv_heads, worker, gridDim.x, [&](int u, int to, auto &&take) {
+    const Place place = find_place<ManyShares<D, T>>(*reinterpret_cast<PlaceScratch *>(smem), units, a.kv_heads, worker, gridDim.x, [&](int u, int to, auto &&take) {
         if (u >= to) return;
         int s = 0;  // the last sequence that begins at u or before
         for (int n = sequences; n > 1;) {
@@ -697,7 +743,7 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
     int t0 = uniform((int)max(place.start - start - kManySetup, (int64_t)0));
     Keys keys = uniform(many_keys(a, r, group, tile, kRows));
     if (tid == 0)
-        a.many_join[worker] = join_at(place, worker, workers_of(place.total, gridDim.x), start, kManySetup, keys.tiles,
+        a.many_join[worker] = join_at(place, Runs<ManyShares<D, T>>(place.total, gridDim.x), worker, start, kManySetup, keys.tiles,
                                       Join{0, 0, 0, r.q.first, tile * kRows, min(r.q.count * group - tile * kRows, kRows), head, 0});
     bool first = true;
 

@@ -264,6 +264,20 @@ def test_more_sequences_than_lds_holds(dt):
         C.assert_attention_close(o, lse, C.attention_ref(cache, batch, turned, 0, 0.125), dt, 64, 120)
 
 
+@pytest.mark.parametrize("dt,dim,kv", [(BF16, 128, 16), (BF16, 64, 32), (F32, 64, 16), (F32, 128, 4), (BF16, 256, 4)])
+def test_long_lists_of_work(dt, dim, kv):
+    """Row tiles and contexts enough for every workgroup to have several."""
+    batch = C.Batch([2000, 2300, 1900, 700], [200, 129, 256, 1], 64, 1)
+    cache = C.Cache(batch.pages, kv, 64, dim)
+    C.fill(cache, batch, 2)
+    cache.to_gpu()
+    batch.to_gpu()
+    q = C.random_queries(batch, kv, dim, dt, 3)
+    call = C.Attention(cache, batch, q, 0, dim ** -0.5, dt)
+    call.run()
+    C.assert_attention_close(*call.results(), C.attention_ref(cache, batch, q, 0, dim ** -0.5), dt, dim, 2500)
+
+
 def test_very_many_sequences():
     """70000 of them, of which four bring a token."""
     count = 70000
