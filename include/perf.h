@@ -371,7 +371,8 @@ perf_status perf_cache_append_fp8(const void *q, const void *k, const void *v, c
  *              contents are scratch; calls that may run at the same time need one each
  *   max_tokens the most new tokens that a sequence brings (of one that brings more the first max_tokens are computed)
  *   window     keys that a query sees at most, itself included; 0 = all
- * What one block of scale 255 holds may turn every query of its sequence in the call to NaN.
+ * A block of scale 255 or a value that is no finite number, among the keys that a sequence's queries of the call see, may turn all
+ * of them to NaN.  What lies elsewhere (before the window, behind the last token, in pages that are not there) counts for nothing.
  * The workspace's size is -1 for arguments that the call would reject.
  * Errors: NULL (all but lse), SHAPE (as perf_cache_append_fp8; max_tokens < 1, window < 0 or > 2^30, scale not finite), DTYPE,
  * ALIGN, UNSUPPORTED (head_dim or page_size as above, tokens * (q_heads/kv_heads) > 2^30), LAUNCH. */

@@ -171,10 +171,11 @@ __device__ __forceinline__ rsrc_t block_rsrc(const uint8_t *pages, const Attenti
     return make_rsrc(pages + (block << a.t.page_shift) * D, page < 0 ? 0 : (uint32_t)D << a.t.page_shift);
 }
 
-// The part of a sequence that a call computes, with its keys [begin, end); begin is on a border of 32.
+// The part of a sequence that a call computes, with its keys [begin, end); begin is on a border of 32, and keys below `low` are
+// none: no query sees them, and what lies in their places may be no number, under any scale.
 struct Span {
     Sequence q;
-    int begin, end;
+    int begin, low, end;
 };
 __device__ __forceinline__ Span span(const AttentionArgs &a, Sequence q)
 {
@@ -182,13 +183,14 @@ __device__ __forceinline__ Span span(const AttentionArgs &a, Sequence q)
     r.q = q;
     r.q.count = min(r.q.count, a.max_tokens);
     r.end = (int)min((int64_t)r.q.held + r.q.count, (int64_t)a.t.columns << a.t.page_shift);
-    r.begin = a.window ? max(r.q.held - a.window + 1, 0) & ~31 : 0;
+    r.low = a.window ? max(r.q.held - a.window + 1, 0) : 0;
+    r.begin = r.low & ~31;
     return r;
 }
 __device__ __forceinline__ Span span(const AttentionArgs &a, int s) { return span(a, sequence(a.t, s)); }
 __device__ __forceinline__ Span uniform(Span r)
 {
-    return Span{Sequence{uniform(r.q.first), uniform(r.q.count), uniform(r.q.held)}, uniform(r.begin), uniform(r.end)};
+    return Span{Sequence{uniform(r.q.first), uniform(r.q.count), uniform(r.q.held)}, uniform(r.begin), uniform(r.low), uniform(r.end)};
 }
 
 // A kernel's tiles, of all items one after the other, are cut into one run for each worker, and none is empty: as many workers as
@@ -414,7 +416,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
     uint32_t scales;  // bytes: K and V of the first half, K and V of the second
     const auto look_up_pages = [&](int base) {
         const int i = base + lane, k = from + i * kFewKeys;
-        page0 = i < n && k < r.end ? page_at(a.t, s, k >> shift) : -1;
+        page0 = i < n && k < r.end && k + 16 > r.low ? page_at(a.t, s, k >> shift) : -1;
         page1 = i < n && k + 16 < r.end ? page_at(a.t, s, (k + 16) >> shift) : -1;
     };
     const auto look_up_scales = [&] {
@@ -431,7 +433,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
     };
     begin();
     while (n > 0) {
-        const int rows = r.q.count * group, held = r.q.held, end = r.end;
+        const int rows = r.q.count * group, held = r.q.held, low = r.low, end = r.end;
         const int token = token_of(a, col, group), position = held + token, last = held + r.q.count - 1;
         asm volatile("" : "+v"(page0), "+v"(page1));
 
@@ -532,14 +534,15 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
                     }
                 }
             }
-            int keep[2] = {-1, -1};  // bytes of V that are keys
+            int keep[2] = {-1, -1};  // bytes of V that are keys (a weight of zero does not cancel a NaN)
             if (now.pages != 3 || k + 31 > held || (a.window && k <= last - a.window)) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int key = k + 16 * h + 4 * g + e;
-                        const bool there = key < end && (now.pages >> h & 1), seen = there && key <= position && (!a.window || key > position - a.window);
+                        const bool there = key >= low && key < end && (now.pages >> h & 1);
+                        const bool seen = there && key <= position && (!a.window || key > position - a.window);
                         if (!there) keep[h] &= ~(255 << (8 * e));
                         sc[h][e] = seen ? sc[h][e] : -INFINITY;
                     }
@@ -670,17 +673,18 @@ template <int D> __device__ __forceinline__ constexpr int turn_many_v(int r)
 __device__ __forceinline__ int many_start(int first, int group, int rows, int s) { return s == 0 ? 0 : (int)((int64_t)first * group / rows) + s; }
 inline int64_t many_units(int64_t tokens, int64_t sequences, int64_t group, int rows) { return tokens * group / rows + sequences; }
 
-// The keys that a row tile needs: [begin, end), begin on a border of 64
-struct Keys { int begin, end, tiles; };
-__device__ __forceinline__ Keys uniform(Keys k) { return Keys{uniform(k.begin), uniform(k.end), uniform(k.tiles)}; }
+// The keys that a row tile needs: [begin, end), begin on a border of 64, and those below `low` none as above
+struct Keys { int begin, low, end, tiles; };
+__device__ __forceinline__ Keys uniform(Keys k) { return Keys{uniform(k.begin), uniform(k.low), uniform(k.end), uniform(k.tiles)}; }
 __device__ __forceinline__ Keys many_keys(const AttentionArgs &a, const Span &r, int group, int tile, int tile_rows)
 {
     const int rows = r.q.count * group, row = tile * tile_rows;
-    Keys k{0, 0, 0};
+    Keys k{0, 0, 0, 0};
     if (row >= rows || is_few(a, r.q.count)) return k;
     const int token0 = token_of(a, row, group), token1 = token_of(a, min(row + tile_rows, rows) - 1, group);
     k.end = (int)min((int64_t)r.q.held + token1 + 1, (int64_t)a.t.columns << a.t.page_shift);
-    k.begin = a.window ? max(r.q.held + token0 - a.window + 1, 0) & ~(kManyKeys - 1) : 0;
+    k.low = a.window ? max(r.q.held + token0 - a.window + 1, 0) : 0;
+    k.begin = k.low & ~(kManyKeys - 1);
     k.tiles = max((k.end - k.begin + kManyKeys - 1) / kManyKeys, 1);
     return k;
 }
@@ -756,7 +760,7 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
     int n, from;
     const auto look_up_page = [&](Pieces &p, int i) {
         const int k = from + i * kManyKeys + 16 * lane;
-        p.page = k < keys.end ? page_at(a.t, s, k >> shift) : -1;
+        p.page = k < keys.end && k + 16 > keys.low ? page_at(a.t, s, k >> shift) : -1;
     };
     const auto look_up_scales = [&](Pieces &p) {
         const int64_t block = (int64_t)p.page * a.kv_heads + head;
@@ -771,7 +775,7 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
     };
     begin();
     while (n > 0) {
-        const int held = r.q.held, end = keys.end, rows = r.q.count * group;
+        const int held = r.q.held, low_key = keys.low, end = keys.end, rows = r.q.count * group;
         const int row0 = tile * kRows + 32 * wave, row = min(row0 + col, rows - 1);  // this wave's first row, and this lane's
         const bool active = row0 < rows;
         const int token = token_of(a, row, group), of_group = row - token * group, position = held + token;
@@ -846,12 +850,12 @@ __global__ __launch_bounds__(256, (many_per_cu<D, T>())) void cache_attention_ma
                     in = stage;
                     stage = stage + kStage == kManyStages * kStage ? 0 : stage + kStage;
                     there = (of.scales0 & of.scales1 & of.scales2 & of.scales3) >> 16;
-                    if (!there || k + kManyKeys > end) {
-                        // values that are not there: zeros, whatever lies in their places (a weight of zero does not cancel a NaN)
+                    if (!there || k < low_key || k + kManyKeys > end) {
+                        // values that are not there or that no row sees: zeros, whatever lies in their places (a weight of zero does not cancel a NaN)
                         const uint32_t s0 = of.scales0, s1 = of.scales1, s2 = of.scales2, s3 = of.scales3, piece = wave < 2 ? (wave == 0 ? +s0 : +s1) : (wave == 2 ? +s2 : +s3);
                         for (int j = lane; j < D; j += 64) {  // this wave's 16 keys, 16 bytes at a time
                             const int key = 16 * wave + j / (D / 16);
-                            if (!(piece >> 16) || k + key >= end) *reinterpret_cast<uint4_t *>(smem + in + (kManyKeys + 16 * wave) * D + 16 * j) = uint4_t{0, 0, 0, 0};
+                            if (!(piece >> 16) || k + key < low_key || k + key >= end) *reinterpret_cast<uint4_t *>(smem + in + (kManyKeys + 16 * wave) * D + 16 * j) = uint4_t{0, 0, 0, 0};
                         }
                         wait_lds();
                         wg_barrier();
