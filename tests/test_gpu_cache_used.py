@@ -240,6 +240,33 @@ def test_rows_beyond_32_bits(held):
         C.assert_attention_close(o, None, C.attention_ref(cache, batch, x, 0, 0.125), BF16, dim, held + 2)
 
 
+@pytest.mark.parametrize("held", [20, 0])
+@pytest.mark.parametrize("heads", [8, 16])
+def test_rows_of_several_heads_beyond_32_bits(held, heads):
+    """Two tokens 2^31 elements apart, whose heads share one of the cache: 16 rows to it are few, 32 many."""
+    ld, dim = 2 ** 31 + 64, 64
+    batch = C.Batch([held], [2], 16, 1)
+    cache = C.Cache(batch.pages, 1, 16, dim)
+    C.fill(cache, batch, 2)
+    cache.to_gpu()
+    batch.to_gpu()
+    q = C.random_queries(batch, heads, dim, BF16, 3)
+    width = heads * dim
+    far, out = (torch.empty(ld + width, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    far[:width], far[ld:] = q[0].flatten().cuda(), q[1].flatten().cuda()
+    out[width:2 * width] = 7.0  # behind the first row
+    lse = torch.empty((2, heads), device="cuda")
+    c = cache.gpu
+    ws = torch.empty(perf.perf_cache_attention_fp8_workspace_bytes(2, 1, 2, heads, 1, dim, 16, batch.columns), dtype=torch.uint8, device="cuda")
+    perf.perf_cache_attention_fp8(far.data_ptr(), c["k"].data_ptr(), c["v"].data_ptr(), c["ks"].data_ptr(), c["vs"].data_ptr(), *batch.addresses(),
+                                  out.data_ptr(), lse.data_ptr(), ws.data_ptr(), 2, 1, 2, heads, 1, dim, ld, ld, cache.pages, 16, batch.columns,
+                                  batch.table.shape[1], 0, 0.125, BF16, stream=G.stream())
+    torch.cuda.synchronize()
+    o = torch.stack((out[:width].cpu(), out[ld:].cpu())).view(2, heads, dim)
+    C.assert_attention_close(o, lse.cpu(), C.attention_ref(cache, batch, q, 0, 0.125), BF16, dim, held + 2)
+    assert bool((out[width:2 * width] == 7.0).all())
+
+
 @pytest.mark.parametrize("dt", [BF16, F32])
 def test_more_sequences_than_lds_holds(dt):
     """700 sequences, of which some bring nothing, one token, or a run."""
