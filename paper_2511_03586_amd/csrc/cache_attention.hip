@@ -286,8 +286,9 @@ __device__ __forceinline__ Place find_place(PlaceScratch &at, int items, int cop
 }
 
 // A tile of rows takes some places of the list before those of its tiles of keys: what a workgroup spends on its beginning and
-// end, in tiles of keys.  (With none, 64 sequences of 64 to 32768 tokens took 165 us where 64 of 5242 took 125: workgroups that
-// met short sequences met many.)
+// end, in tiles of keys.  (With none, 64 sequences of 64 to 32768 tokens took 160-165 us, for 134 so, where 64 of 5242 took 125:
+// workgroups that met short sequences met many.)  Lists so short that a run has fewer places than a setup leave workgroups without
+// keys: 53 of 256 where six sequences bring 39 tiles of keys to each of ten heads.
 constexpr int kFewSetup = 3, kManySetup = 5;
 
 // What has to be joined where the run of `worker` begins, in a tile of rows whose places, `setup` and `tiles`, begin with `start`
@@ -336,8 +337,8 @@ struct Sequences {
 // no trip to memory.
 //
 // 64 sequences of 64 to 32768 tokens, 8 heads of 128, 32 queries: 134 us, 5.4 TB/s (a copy of 1 GiB reaches 6.4); one of 131071
-// tokens 55 us, 5.1 TB/s; 16 of 2048 to 6000 tokens 29-31 us, 4.1 TB/s, the beginning (4.7 us: lengths, then pages, then keys) and
-// the waits where heads end being the rest.
+// tokens 55 us, 5.1 TB/s; 16 of 2048 to 6000 tokens 30-31 us, 4.0 TB/s, of which 10 pass before the first key (lengths, then the run's
+// place, then pages, then keys) and 11 with the eight tiles of a run.
 //
 // S^T = K Q^T and o^T = V^T P^T on v_mfma_f32_16x16x32_bf16, queries in the columns: a lane has one query, keys 4 g .. 4 g + 3 of
 // both halves of the 32 (g = lane / 16), whose weights are its share of the second product's operand as they are.  The rows of V
@@ -636,25 +637,28 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_few_ker
 // each wave has 32 of the rows.  The blocks of all row tiles and heads are one list, cut into equal runs as above, heads first: an
 // XCD's workgroups take neighbouring runs, which share keys in its L2.
 //
-// 4 prompts of about 2048 tokens, 8 heads of 128, 32 queries: 212-221 us, 0.65 PFLOP/s of what is seen (a large library product in
-// bf16: 1.2).  Beside the 32 products of a wave and block (0.48 us) stand some 320 vector instructions for widening keys and values,
-// exponentials and maxima, which two waves of a SIMD hide from each other in part: 0.84 us a block and SIMD where
-// contexts are long, and beginnings and ends of row tiles, five to a workgroup, take as long again as their blocks here.  64 rows to a wave, which
-// widens half as often, leave one wave to a SIMD: 334 us.  Keys widened once for two waves, weights through LDS: 240 us.
+// 4 prompts of about 2048 tokens, 8 heads of 128, 32 queries: 208-230 us, 0.60-0.66 PFLOP/s of what is seen (a large library product
+// in bf16: 1.2).  Beside the 32 products of a wave and block (0.49 us) stand some 320 vector instructions for widening keys and
+// values, exponentials and maxima, which two waves of a SIMD hide from each other in part: 1.15 us a block and SIMD, by what a
+// longer context adds.  Blocks are two thirds of the time here, beginnings and ends of row tiles, five to a workgroup, the rest.
+// 64 rows to a wave, which widen half as often, leave one wave to a SIMD: 334 us.  Keys widened once for two waves, weights
+// through LDS: 240 us.  With fp32 queries, for the same operations, 506 us (heads of 64: 302, half the operations; of 256: 497, though
+// 71 registers of a lane go to memory there); heads of 256 in bf16, one wave to a SIMD, 246.
 //
 // The products are those above on v_mfma_f32_32x32x16_bf16: a lane has one query, and keys 4 g .. 4 g + 3 of every eight (g =
 // lane / 32).  The weights of bf16 queries are rounded to bf16 once (the few rows' kernel, which waits for memory, keeps 16 bits
-// of them): another product with what that leaves would cost half of the time again.  A running maximum is raised only by more
+// of them): another product with what that leaves makes 214 us 274 (20 mixed sequences 162 -> 201, 32 of 512 tokens 71 -> 79), and
+// the error against 64 bits 0.0019 instead of 0.00166, most of which is the rounding of o.  A running maximum is raised only by more
 // than 2^8 in weights, which fp32 sums carry as well: the sums are then seldom scaled.
 constexpr int kManyKeys = 64, kManyStages = 3;
 constexpr int kManyRows = 128;
 // workgroups to a CU, by the registers that a wave needs for its queries and sums
 template <int D, typename T> constexpr int many_per_cu() { return D == 256 || (D == 128 && sizeof(T) == 4) ? 1 : D == 64 && sizeof(T) == 2 ? 3 : 2; }
 // Of workgroups that share a CU the one that came first is served first: with equal runs it ended after 167 us and the second after
-// 217 (4 prompts of about 2048 tokens, heads of 128), and the second's waves, then alone, hide nothing.  With these shares 228-235
-// us became 212-221 for the kernel, 137 -> 130 for 20 mixed ones, and with three to a CU (32 x 512, heads of 64) 67 -> 60; 6 : 5 and 3 : 2
-// are slower.  Contexts of some thousand tokens under each prompt lose 2 % (790 -> 805 us for 4 x 2048 on 4096).  The kernel for few
-// rows, which waits for memory, gains nothing by it.
+// 217 (4 prompts of about 2048 tokens, heads of 128), and the second's waves, then alone, hide nothing.  Equal runs, then these, a call:
+// 4 x 2048 tokens 228 -> 216 us, on 1024 tokens 378 -> 361, on 4096 827 -> 803; with three to a CU (heads of 64) 32 x 512 80 -> 70, on
+// 2048 276 -> 260.  6 : 5 and 3 : 2 are slower.  8 x 512 on 8192, whose row tiles have 129 blocks and more, lose: 675 -> 686.  The
+// kernel for few rows, which waits for memory, gains nothing by it.
 template <int D, typename T>
 using ManyShares = std::conditional_t<many_per_cu<D, T>() == 1, Shares<1>, std::conditional_t<many_per_cu<D, T>() == 2, Shares<4, 3>, Shares<7, 4, 3>>>;
 template <int D, typename T> constexpr int many_workers() { return 256 * many_per_cu<D, T>(); }
